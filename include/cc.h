@@ -33,6 +33,8 @@
  *   cc_chunk_attention inter / intra attention sums between the segments of a prompt (Eq. (2), (3));
  *                      cc_chunk_ab / cc_chunk_cci / cc_chunk_reuse: CCI, beta, gamma, beta', CFO and
  *                      the token budget from them on the host (Sec. 3.1, 3.3)
+ *   cc_extend_segments, cc_append_attention, cc_sample  the answer that follows the prefill: tables of the
+ *                      next rows on the GPU, their attention over the merged paged KV, the next token
  *
  * Conventions
  *   - Every tensor and every metadata array is DEVICE memory owned by the caller; the library
@@ -459,6 +461,83 @@ int cc_chunk_attention(cc_ctx* ctx, const void* q, const int32_t* q_pos, const i
                        const int32_t* req_seg_off, int32_t n_requests, int32_t n_ctx_tokens,
                        int32_t n_pairs, const float* lse, float* pair_mass, float* self_mass,
                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- (f) tables of new rows -------------------------------------------------------------------
+ * Every segment s of the batch holds segs_in[s].n_tokens tokens (their keys and values are in its pages) and
+ * gets n_new[s] more behind them (negative: none).  A segment in front of others of its request may grow only while
+ * those are empty (the positions of what is cached are fixed).  From nothing (n_tokens = 0, n_new = the lengths)
+ * the call lays out whole prompts; with one new token in each request's last segment it is a step of an answer.
+ *   segs [n_segs]: segs_in (may be the same array) with
+ *       req = the request r whose [req_seg_off[r], req_seg_off[r + 1]) holds s,  n_tokens = old + new,
+ *       logical_start = sum of n_tokens of the request's earlier segments,
+ *       n_select = new, sel_off = sum of n_select of all earlier segments of the batch,
+ *       tok_off = sum of n_tokens of all earlier segments of the batch;  kind and tab_off as they are.
+ *   block_tab [n_tab], updated in place: segment s owns the tab_cap[s] entries from tab_off on, and its first
+ *       ceil(old / 16) hold pages.  The pages it needs besides come from the front of free_blocks [n_free], in
+ *       the order of the segments; counts[1] of them are taken.  Other entries are left alone.
+ *   cu_q [n_requests + 1]: row offsets of the requests.  For row j < cu_q[n_requests], in the order of the
+ *       segments and their tokens:  q_pos[j] = position, slot_map[j] = page * 16 + t % 16 of token t of its segment
+ *       (-1 if the page is not in [0, n_blocks)), row_req[j] = request;  for the rows behind, up to max_rows
+ *       (the size of the three arrays): 0, -1, -1, so that a call over max_rows rows writes nothing for them.
+ *   last_row [n_requests]: the request's last row, -1 if it has none (the row whose logits are sampled).
+ *   status [n_requests]: CC_EXTEND_OK, or why the request gets NOTHING in this call: a segment's entries do not
+ *       hold its pages (or the request would reach 2^31 tokens), a segment in front of cached tokens grows,
+ *       or the pages / rows of all requests up to and including it (the refused ones' wishes count) exceed
+ *       n_free / max_rows.  A request that needs no page is not refused for pages.
+ *   counts [4]: rows, pages taken, requests refused, tokens of all segments (must stay below 2^31).
+ *   workspace: cc_extend_segments_workspace_bytes(ctx, n_segs, n_requests). */
+enum { CC_EXTEND_OK = 0, CC_EXTEND_NO_PAGES = 1, CC_EXTEND_TABLE_FULL = 2, CC_EXTEND_ORDER = 3, CC_EXTEND_NO_ROWS = 4 };
+size_t cc_extend_segments_workspace_bytes(const cc_ctx* ctx, int32_t n_segs, int32_t n_requests);
+int cc_extend_segments(cc_ctx* ctx, const cc_segment* segs_in, const int32_t* n_new, const int32_t* tab_cap, int32_t n_segs,
+                       const int32_t* req_seg_off, int32_t n_requests, const int32_t* free_blocks, int32_t n_free,
+                       int32_t* block_tab, int32_t n_tab, int32_t n_blocks, cc_segment* segs, int32_t* cu_q, int32_t* q_pos,
+                       int32_t* slot_map, int32_t* row_req, int32_t max_rows, int32_t* last_row, int32_t* status,
+                       int32_t* counts, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- (g) attention of new rows over the paged context ------------------------------------------
+ * cc_sparse_prefill for the rows of an answer: one per request while it is written, several for a draft that is
+ * checked at once, some hundred for a further question over a long context.  The same two steps and the same
+ * arguments (rows, positions and slots from cc_extend_segments or any list cc_sparse_prefill takes), but the KEYS are
+ * divided over workgroups, and the parts joined, so that a few rows of a long context fill the chip.
+ *   Rows [cu_q[n_requests], n_q_tot) are not attended and their out and lse stay as they are; rows whose slot lies
+ *   outside the pool are attended but not written.  A row that sees no key gets zeros and lse = -infinity.
+ *   What lies in a masked place (padding slots, keys behind the row, pages outside the pool) changes nothing, NaN
+ *   and infinities included.
+ *   max_q_per_req: at least the rows of any request (host scalar; bounds the grid).
+ *   max_ctx_tokens, max_segs_per_req: tokens and segments of the largest request (host scalars, upper bounds; they
+ *   decide how the keys are divided, not what is read).  lse may be NULL; shared as for cc_sparse_prefill.
+ *   The sums' order depends on n_requests, max_q_per_req, max_ctx_tokens and max_segs_per_req, on nothing else.
+ *   workspace: cc_append_attention_workspace_bytes(ctx, n_q_tot, max_q_per_req, n_requests, max_ctx_tokens,
+ *   max_segs_per_req). */
+size_t cc_append_attention_workspace_bytes(const cc_ctx* ctx, int32_t n_q_tot, int32_t max_q_per_req, int32_t n_requests,
+                                           int32_t max_ctx_tokens, int32_t max_segs_per_req);
+int cc_append_attention(cc_ctx* ctx, const void* q, const void* k_new, const void* v_new, const int32_t* src_rows,
+                        const int32_t* q_pos, const int32_t* slot_map, const int32_t* cu_q, int32_t n_q_tot,
+                        int32_t max_q_per_req, void* k_pool, void* v_pool, int32_t n_blocks, const int32_t* block_tab,
+                        const cc_segment* segs, int32_t n_segs, const int32_t* req_seg_off, int32_t n_requests,
+                        int32_t max_ctx_tokens, int32_t max_segs_per_req, const cc_shared_values* shared, void* out,
+                        float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- (h) the next token ------------------------------------------------------------------------
+ * One token per row r of logits z [n_rows][stride] (the first n_vocab columns; logits_dtype CC_F32 or CC_BF16,
+ * whatever the context's), from a given uniform number u[r] in [0, 1):
+ *   w_i = exp((z_i - max z) / temperature[r]).  The tokens are ranked by logit, the lower index first among equals.
+ *   Kept are the ranks that pass all of
+ *     top_k:  rank < top_k[r]                                           (0, negative or > n_vocab: off)
+ *     top_p:  weight of the ranks in front < top_p[r] * weight of the ranks that pass top_k     (1 or more: off)
+ *     min_p:  w_i >= min_p[r]                                           (0 or less: off)
+ *   and rank 0 in any case.  token[r] = the first kept token i, by index, with  sum_{kept j <= i} w_j > u[r] * sum_kept w.
+ *   temperature[r] <= 0: the largest logit (lowest index), whatever the other settings.
+ *   logprob[r] = log(w_token / sum_kept w);  n_kept[r] = number of kept tokens.
+ * -infinity and NaN are never kept; a row of nothing else gives token -1, logprob -infinity, n_kept 0.  Beside +infinity
+ * every finite logit has weight 0.  u below 0 or NaN counts as 0, u of 1 or more as the largest float below 1.
+ * NULL turns off: temperature (1 then), top_k, top_p, min_p, logprob, n_kept.  All [n_rows].
+ * Weights are taken in 64 bits and summed as whole numbers, so that the result does not depend on how the work is divided.
+ *   workspace: cc_sample_workspace_bytes(ctx, n_rows, n_vocab). */
+size_t cc_sample_workspace_bytes(const cc_ctx* ctx, int32_t n_rows, int32_t n_vocab);
+int cc_sample(cc_ctx* ctx, const void* logits, int32_t logits_dtype, int32_t n_rows, int32_t n_vocab, int64_t stride,
+              const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
+              int32_t* token, float* logprob, int32_t* n_kept, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- reuse scores of a chunk-cache (host only; no GPU work, HOST pointers) --------------------
  * cc_chunk_ab: one layer's a(C_i) = sum_{j<i} inter(C_j, C_i) / (|C_i| |C_j|) and

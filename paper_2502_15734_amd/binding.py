@@ -122,6 +122,20 @@ def load_library() -> C.CDLL:
     lib.cc_chunk_attention.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp, i32, vp, vp, i32, vp, i32, i32, i32,
                                        vp, vp, vp, vp, sz, vp]
     lib.cc_chunk_attention.restype = C.c_int
+    lib.cc_extend_segments_workspace_bytes.argtypes = [vp, i32, i32]
+    lib.cc_extend_segments_workspace_bytes.restype = sz
+    lib.cc_extend_segments.argtypes = [vp, vp, vp, vp, i32, vp, i32, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp,
+                                       vp, sz, vp]
+    lib.cc_extend_segments.restype = C.c_int
+    lib.cc_append_attention_workspace_bytes.argtypes = [vp, i32, i32, i32, i32, i32]
+    lib.cc_append_attention_workspace_bytes.restype = sz
+    lib.cc_append_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, i32, vp, vp, i32, vp, i32, i32, i32,
+                                        vp, vp, vp, vp, sz, vp]
+    lib.cc_append_attention.restype = C.c_int
+    lib.cc_sample_workspace_bytes.argtypes = [vp, i32, i32]
+    lib.cc_sample_workspace_bytes.restype = sz
+    lib.cc_sample.argtypes = [vp, vp, i32, i32, i32, C.c_int64, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.cc_sample.restype = C.c_int
     dp = C.POINTER(C.c_double)
     lib.cc_chunk_ab.argtypes = [dp, C.POINTER(i32), i32, C.c_double, i32, dp, dp]
     lib.cc_chunk_ab.restype = C.c_int
@@ -413,6 +427,56 @@ class Context:
             k_pool.shape[0], _ptr(block_tab), _ptr(segs), segs.shape[0], _ptr(req_seg_off), n_requests,
             n_ctx_tokens, _ptr(lse), _ptr(seg_mass), _ptr(workspace),
             workspace.numel() * workspace.element_size(), _stream()))
+
+    # -- cc_extend_segments --------------------------------------------------------------------
+    def extend_segments_workspace_bytes(self, n_segs: int, n_requests: int) -> int:
+        return int(self._lib.cc_extend_segments_workspace_bytes(self._h, n_segs, n_requests))
+
+    def extend_segments(self, segs_in, n_new, tab_cap, req_seg_off, free_blocks, block_tab, n_blocks, segs, cu_q, q_pos, slot_map,
+                        row_req, last_row, status, counts, workspace):
+        """Tables of n_new[s] tokens behind what segment s holds; n_blocks: size of the pool the pages belong to.  segs may be segs_in."""
+        n_segs, n_requests, max_rows = segs_in.shape[0], req_seg_off.shape[0] - 1, q_pos.shape[0]
+        if not (segs.shape[0] == n_new.shape[0] == tab_cap.shape[0] == n_segs and slot_map.shape[0] == row_req.shape[0] == max_rows
+                and cu_q.shape[0] == n_requests + 1 and last_row.shape[0] == status.shape[0] == n_requests and counts.shape[0] >= 4):
+            raise ValueError("extend_segments: tensors of different lengths")
+        self._check(self._lib.cc_extend_segments(
+            self._h, _ptr(segs_in), _ptr(n_new), _ptr(tab_cap), n_segs, _ptr(req_seg_off), n_requests, _ptr(free_blocks),
+            free_blocks.shape[0], _ptr(block_tab), block_tab.shape[0], n_blocks, _ptr(segs), _ptr(cu_q), _ptr(q_pos), _ptr(slot_map),
+            _ptr(row_req), max_rows, _ptr(last_row), _ptr(status), _ptr(counts), _ptr(workspace), _nbytes(workspace), _stream()))
+
+    # -- cc_append_attention -------------------------------------------------------------------
+    def append_attention_workspace_bytes(self, n_q_tot: int, max_q_per_req: int, n_requests: int, max_ctx_tokens: int,
+                                         max_segs_per_req: int) -> int:
+        return int(self._lib.cc_append_attention_workspace_bytes(self._h, n_q_tot, max_q_per_req, n_requests, max_ctx_tokens,
+                                                                 max_segs_per_req))
+
+    def append_attention(self, q, k_new, v_new, q_pos, slot_map, cu_q, max_q_per_req, k_pool, v_pool, block_tab, segs, req_seg_off,
+                         n_requests, max_ctx_tokens, max_segs_per_req, out, lse, workspace, src_rows=None, shared=None):
+        """sparse_prefill for the rows of an answer: the keys are divided over the chip.  lse: tensor or None."""
+        n_q_tot = q.shape[0] if src_rows is None else src_rows.shape[0]
+        self._check(self._lib.cc_append_attention(
+            self._h, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(src_rows), _ptr(q_pos), _ptr(slot_map), _ptr(cu_q), n_q_tot,
+            max_q_per_req, _ptr(k_pool), _ptr(v_pool), k_pool.shape[0], _ptr(block_tab), _ptr(segs), segs.shape[0], _ptr(req_seg_off),
+            n_requests, max_ctx_tokens, max_segs_per_req, _shared(shared), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace),
+            _stream()))
+
+    # -- cc_sample -----------------------------------------------------------------------------
+    def sample_workspace_bytes(self, n_rows: int, n_vocab: int) -> int:
+        return int(self._lib.cc_sample_workspace_bytes(self._h, n_rows, n_vocab))
+
+    def sample(self, logits, n_vocab, u, token, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, n_kept=None,
+               workspace=None):
+        """One token per row of logits [rows, columns >= n_vocab] (float32 or bfloat16) from the uniform numbers u."""
+        if logits.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("sample: logits in float32 or bfloat16")
+        n_rows = logits.shape[0]
+        for t in (u, token, temperature, top_k, top_p, min_p, logprob, n_kept):
+            if t is not None and t.shape[0] < n_rows:
+                raise ValueError("sample: a tensor has fewer entries than there are rows")
+        self._check(self._lib.cc_sample(
+            self._h, _ptr(logits), CC_BF16 if logits.dtype == torch.bfloat16 else CC_F32, n_rows, n_vocab, logits.shape[1],
+            _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(token), _ptr(logprob), _ptr(n_kept), _ptr(workspace),
+            _nbytes(workspace), _stream()))
 
 
 # ---- host-only reuse scores (Sec. 3.1, 3.3) ------------------------------------------------------

@@ -642,4 +642,96 @@ int cc_chunk_attention(cc_ctx* ctx, const void* q, const int32_t* q_pos, const i
   return cc::check_launch(ctx, fn);
 }
 
+size_t cc_extend_segments_workspace_bytes(const cc_ctx* ctx, int32_t n_segs, int32_t n_requests) {
+  if (ctx == nullptr || n_segs < 0 || n_requests < 0) return 0;
+  return cc::align_up(cc::extend_bytes(n_segs, n_requests), 256);
+}
+
+int cc_extend_segments(cc_ctx* ctx, const cc_segment* segs_in, const int32_t* n_new, const int32_t* tab_cap, int32_t n_segs,
+                       const int32_t* req_seg_off, int32_t n_requests, const int32_t* free_blocks, int32_t n_free,
+                       int32_t* block_tab, int32_t n_tab, int32_t n_blocks, cc_segment* segs, int32_t* cu_q, int32_t* q_pos,
+                       int32_t* slot_map, int32_t* row_req, int32_t max_rows, int32_t* last_row, int32_t* status,
+                       int32_t* counts, void* workspace, size_t workspace_bytes, void* stream) {
+  static const char* fn = "cc_extend_segments";
+  if (ctx == nullptr) return CC_ERR_INVALID_ARG;
+  CC_REQUIRE(n_segs >= 0 && n_requests >= 0 && n_free >= 0 && n_tab >= 0 && n_blocks >= 0 && max_rows >= 0, "negative count");
+  CC_REQUIRE(n_segs <= 65535 && n_requests <= 65535, "more than 65535 segments or requests in one call");
+  CC_REQUIRE(n_blocks <= (1 << 27) - 1, "a pool of more than 2^27 - 1 blocks has slots beyond 32 bits");
+  if (n_requests == 0) return CC_OK;
+  CC_REQUIRE(req_seg_off && cu_q && last_row && status && counts, "null pointer");
+  CC_REQUIRE(n_segs == 0 || (segs_in && segs && n_new && tab_cap), "null pointer");
+  CC_REQUIRE((n_free == 0 || free_blocks) && (n_tab == 0 || block_tab) && (max_rows == 0 || (q_pos && slot_map && row_req)), "null pointer");
+  CC_REQUIRE(aligned16(segs_in) && aligned16(segs), "segment tables must be 16-byte aligned");
+  CC_REQUIRE(workspace != nullptr && aligned16(workspace), "workspace missing or misaligned");
+  if (workspace_bytes < cc_extend_segments_workspace_bytes(ctx, n_segs, n_requests))
+    return fail(ctx, CC_ERR_WORKSPACE_TOO_SMALL, "cc_extend_segments: workspace smaller than cc_extend_segments_workspace_bytes()");
+  cc::launch_extend_segments(segs_in, n_new, tab_cap, n_segs, req_seg_off, n_requests, free_blocks, n_free, block_tab, n_tab, n_blocks, segs,
+                             cu_q, q_pos, slot_map, row_req, max_rows, last_row, status, counts, workspace, static_cast<hipStream_t>(stream));
+  return cc::check_launch(ctx, fn);
+}
+
+size_t cc_append_attention_workspace_bytes(const cc_ctx* ctx, int32_t n_q_tot, int32_t max_q_per_req, int32_t n_requests,
+                                           int32_t max_ctx_tokens, int32_t max_segs_per_req) {
+  if (ctx == nullptr || n_q_tot < 0 || max_q_per_req < 0 || n_requests < 0 || max_ctx_tokens < 0 || max_segs_per_req < 0) return 0;
+  return cc::align_up(cc::append_bytes(ctx, n_q_tot, max_q_per_req, n_requests, max_ctx_tokens, max_segs_per_req), 256);
+}
+
+int cc_append_attention(cc_ctx* ctx, const void* q, const void* k_new, const void* v_new, const int32_t* src_rows,
+                        const int32_t* q_pos, const int32_t* slot_map, const int32_t* cu_q, int32_t n_q_tot,
+                        int32_t max_q_per_req, void* k_pool, void* v_pool, int32_t n_blocks, const int32_t* block_tab,
+                        const cc_segment* segs, int32_t n_segs, const int32_t* req_seg_off, int32_t n_requests,
+                        int32_t max_ctx_tokens, int32_t max_segs_per_req, const cc_shared_values* shared, void* out,
+                        float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  static const char* fn = "cc_append_attention";
+  if (ctx == nullptr) return CC_ERR_INVALID_ARG;
+  CC_REQUIRE(n_q_tot >= 0 && max_q_per_req >= 0 && n_segs >= 0 && n_requests >= 0 && max_ctx_tokens >= 0 && max_segs_per_req >= 0,
+             "negative count");
+  CC_REQUIRE(max_q_per_req <= n_q_tot, "max_q_per_req exceeds n_q_tot");
+  if (n_q_tot == 0) return CC_OK;
+  CC_REQUIRE(q && k_new && v_new && q_pos && slot_map && cu_q && k_pool && v_pool && block_tab && segs && req_seg_off && out, "null pointer");
+  CC_REQUIRE(n_blocks > 0 && n_requests > 0 && n_segs > 0 && max_q_per_req > 0 && max_ctx_tokens > 0 && max_segs_per_req > 0,
+             "sizes must be positive");
+  CC_REQUIRE(n_requests <= 65535, "more than 65535 requests in one call");
+  CC_REQUIRE(n_blocks <= (1 << 27) - 1, "a pool of more than 2^27 - 1 blocks has slots beyond 32 bits");
+  CC_REQUIRE(aligned16(q) && aligned16(k_new) && aligned16(v_new) && aligned16(k_pool) && aligned16(v_pool) && aligned16(out) && aligned16(segs),
+             "tensors must be 16-byte aligned");
+  CC_REQUIRE(q != out, "q and out must not be the same tensor");
+  const size_t need = cc_append_attention_workspace_bytes(ctx, n_q_tot, max_q_per_req, n_requests, max_ctx_tokens, max_segs_per_req);
+  CC_REQUIRE(need == 0 || (workspace != nullptr && aligned16(workspace)), "workspace missing or misaligned");
+  if (workspace_bytes < need)
+    return fail(ctx, CC_ERR_WORKSPACE_TOO_SMALL, "cc_append_attention: workspace smaller than cc_append_attention_workspace_bytes()");
+  cc::ValueSource vs;
+  if (!value_source(ctx, fn, shared, &vs)) return CC_ERR_INVALID_ARG;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  cc::launch_rope_scatter(ctx, cc::ScatterJob{k_new, v_new, src_rows, q_pos, slot_map, n_q_tot, k_pool, v_pool, n_blocks, vs}, st);
+  cc::launch_append_attention(ctx, q, src_rows, q_pos, cu_q, n_q_tot, max_q_per_req, k_pool, v_pool, n_blocks, block_tab, segs, req_seg_off,
+                              n_requests, max_ctx_tokens, max_segs_per_req, out, lse, workspace, st, vs);
+  return cc::check_launch(ctx, fn);
+}
+
+size_t cc_sample_workspace_bytes(const cc_ctx* ctx, int32_t n_rows, int32_t n_vocab) {
+  return ctx == nullptr || n_rows < 0 || n_vocab < 0 ? 0 : cc::align_up(cc::sample_bytes(n_rows, n_vocab), 256);
+}
+
+int cc_sample(cc_ctx* ctx, const void* logits, int32_t logits_dtype, int32_t n_rows, int32_t n_vocab, int64_t stride,
+              const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
+              int32_t* token, float* logprob, int32_t* n_kept, void* workspace, size_t workspace_bytes, void* stream) {
+  static const char* fn = "cc_sample";
+  if (ctx == nullptr) return CC_ERR_INVALID_ARG;
+  CC_REQUIRE(n_rows >= 0 && n_vocab > 0 && stride >= n_vocab, "bad sizes");
+  CC_REQUIRE(n_rows <= 65535, "more than 65535 rows in one call");
+  CC_REQUIRE(n_vocab <= 1 << 22, "more than 2^22 columns");
+  if (logits_dtype != CC_F32 && logits_dtype != CC_BF16) return fail(ctx, CC_ERR_UNSUPPORTED, "cc_sample: unknown dtype of the logits");
+  if (n_rows == 0) return CC_OK;
+  CC_REQUIRE(logits && u && token, "null pointer");
+  CC_REQUIRE(aligned16(logits), "tensors must be 16-byte aligned");
+  const size_t need = cc_sample_workspace_bytes(ctx, n_rows, n_vocab);
+  CC_REQUIRE(need == 0 || (workspace != nullptr && aligned16(workspace)), "workspace missing or misaligned");
+  if (workspace_bytes < need)
+    return fail(ctx, CC_ERR_WORKSPACE_TOO_SMALL, "cc_sample: workspace smaller than cc_sample_workspace_bytes()");
+  cc::launch_sample(logits, logits_dtype, n_rows, n_vocab, stride, temperature, top_k, top_p, min_p, u, token, logprob, n_kept, workspace,
+                    static_cast<hipStream_t>(stream));
+  return cc::check_launch(ctx, fn);
+}
+
 }  // extern "C"
