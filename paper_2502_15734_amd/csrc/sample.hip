@@ -1,10 +1,22 @@
 // cc_sample: one token per row of logits.
 //
 // With x_i = (z_i - max z) / T the weights are w_i = exp(x_i), taken in 64 bits and held as whole multiples of 2^-shift
-// (shift = 62 - ceil(log2 vocab), so that a row's sum stays below 2^62): sums of whole numbers come out the same in every order, so the
+// (shift = min(50, 62 - ceil(log2 vocab)): a row's sum stays below 2^62).  Sums of whole numbers come out the same in every order, so the
 // drawn token does not depend on how a row is divided, and an error of 2^-46 per weight does not move a border that a float would.
-// The kept tokens are the first ranks of the order (logit descending, index ascending); a rank cut is a logit and a number of
-// its ties, found by a radix descent over the logits' ordered bit patterns with counts and weights per digit.
+// The kept tokens are the first ranks of the order (logit descending, index ascending), so every cut is one (logit, index).
+//
+// A row is read by several workgroups (sample_plan): three passes over parts of the row, of which the second and third find it in
+// the caches, and a last kernel with a workgroup per row.
+//   sample_max_kernel    largest and smallest logit of each part
+//   sample_hist_kernel   rows with top-k or top-p: counts and weights per bin of equal width between the largest logit and the smallest
+//                        (or the one whose weight is 2^-66, where that is larger)
+//   sample_tiles_kernel  finds the bin a cut falls into; sums the weights of the bins in front of it per tile of the row, and lists the
+//                        logits of that bin, the candidates
+//   sample_draw_kernel   sorts the candidates, finds the cut among them, the tile the drawn number falls into and the token in it
+// Rows with more candidates than the list holds (thousands of equal logits) are done by the last kernel alone, with radix descents
+// over the whole row; vocabularies that fit the list need no other kernel than the last.
+#include <algorithm>
+
 #include "device_util.h"
 
 namespace cc {
@@ -45,24 +57,49 @@ struct RowSettings {
 __device__ __forceinline__ RowSettings settings_of(const SampleArgs& a, int row) {
   RowSettings s;
   const float t = a.temperature != nullptr ? a.temperature[row] : 1.f;
-  s.greedy = !(t > 0.f);
-  s.inv_t = s.greedy ? 1.0 : 1.0 / static_cast<double>(t);
   const int k = a.top_k != nullptr ? a.top_k[row] : 0;
-  s.top_k = s.greedy ? 1 : (k <= 0 || k > a.vocab) ? a.vocab : k;
   const float p = a.top_p != nullptr ? a.top_p[row] : 1.f, m = a.min_p != nullptr ? a.min_p[row] : 0.f, u = a.u[row];
-  s.top_p = p < 1.f ? fmax(static_cast<double>(p), 0.0) : 1.0;                  // (a NaN: off)
+  s.greedy = !(t > 0.f) || k == 1 || m > 1.f || p <= 0.f;                        // (the largest logit alone)
+  s.inv_t = s.greedy ? 1.0 : 1.0 / static_cast<double>(t);
+  s.top_k = (k <= 0 || k > a.vocab) ? a.vocab : k;
+  s.top_p = p < 1.f ? static_cast<double>(p) : 1.0;                             // (a NaN: off)
   s.min_p = m > 0.f ? static_cast<double>(m) : 0.0;
   s.u = u > 0.f ? fmin(static_cast<double>(u), 1.0 - 0x1p-24) : 0.0;
   return s;
+}
+
+// exp of x <= 0: x = n ln 2 + r, |r| <= ln 2 / 2, the series of exp(r) to r^13 (the rest is below 2^-57)
+__device__ __forceinline__ double exp_of(double x) {
+  x = fmax(x, -800.0);                                 // (0 in 64 bits)
+  const double n = rint(x * 1.4426950408889634074);
+  const double r = fma(n, 0x1.8432a1b0e2634p-43, fma(n, -0x1.62e42fefa4000p-1, x));       // (ln 2 in two parts: its first 40 bits, so that their product is exact, and the rest)
+  double p = 1.0 / 6227020800.0;
+  p = fma(p, r, 1.0 / 479001600.0);
+  p = fma(p, r, 1.0 / 39916800.0);
+  p = fma(p, r, 1.0 / 3628800.0);
+  p = fma(p, r, 1.0 / 362880.0);
+  p = fma(p, r, 1.0 / 40320.0);
+  p = fma(p, r, 1.0 / 5040.0);
+  p = fma(p, r, 1.0 / 720.0);
+  p = fma(p, r, 1.0 / 120.0);
+  p = fma(p, r, 1.0 / 24.0);
+  p = fma(p, r, 1.0 / 6.0);
+  p = fma(p, r, 0.5);
+  p = fma(p, r, 1.0);
+  p = fma(p, r, 1.0);
+  return ldexp(p, static_cast<int>(n));
 }
 
 // weight of a logit against the row's largest one
 __device__ __forceinline__ double weight_of(uint32_t key, uint32_t top, double inv_t) {
   if (key == top) return 1.0;
   if (key <= kKeyNone || top == kKeyInf) return 0.0;
-  return exp((static_cast<double>(logit_of(key)) - static_cast<double>(logit_of(top))) * inv_t);
+  return exp_of((static_cast<double>(logit_of(key)) - static_cast<double>(logit_of(top))) * inv_t);
 }
-__device__ __forceinline__ unsigned long long fixed_of(double w, int shift) { return static_cast<unsigned long long>(ldexp(w, shift) + 0.5); }
+// the nearest multiple of 2^-shift (shift <= 50, w <= 1: the sum with 2^52 has it in its last bits)
+__device__ __forceinline__ unsigned long long fixed_of(double w, int shift) {
+  return static_cast<unsigned long long>(__double_as_longlong(ldexp(w, shift) + 0x1p52) - __double_as_longlong(0x1p52));
+}
 
 template <typename T>
 __device__ __forceinline__ uint32_t key_at(const SampleArgs& a, int row, int i) {
@@ -74,47 +111,23 @@ struct Cut {              // the ranks above it: logits above key, and the first
   unsigned ties;
 };
 
-constexpr int kWaves = 16;
+constexpr int kWaves = 16, kThreads = 64 * kWaves;   // of the kernel with a workgroup per row
 
-// One workgroup per row.
+struct RowShared {
+  unsigned count[256];
+  unsigned long long mass[256];
+  unsigned wave_ties[kWaves], wave_kept[kWaves];
+  unsigned long long wave_mass[kWaves];
+  unsigned found_digit, found_count;
+  unsigned long long found_mass;
+};
+
+// The whole row by one workgroup, whatever its logits.  top: its largest one.
 template <typename T>
-__global__ __launch_bounds__(64 * kWaves) void sample_row_kernel(SampleArgs a) {
-  __shared__ unsigned count[256];
-  __shared__ unsigned long long mass[256];
-  __shared__ uint32_t wave_key[kWaves];
-  __shared__ int wave_idx[kWaves];
-  __shared__ unsigned wave_ties[kWaves], wave_kept[kWaves];
-  __shared__ unsigned long long wave_mass[kWaves];
-  __shared__ unsigned found_digit, found_count;
-  __shared__ unsigned long long found_mass;
-  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = a.vocab;
-  const RowSettings s = settings_of(a, row);
-
-  // ---- the largest logit and its lowest index
-  uint32_t top = 0;
-  int top_idx = 0x7fffffff;
-  for (int i = tid; i < n; i += 64 * kWaves) {
-    const uint32_t k = key_at<T>(a, row, i);
-    if (k > top) { top = k; top_idx = i; }
-  }
-  for (int o = 32; o > 0; o >>= 1) {
-    const uint32_t k = __shfl_xor(top, o, 64);
-    const int i = __shfl_xor(top_idx, o, 64);
-    if (k > top || (k == top && i < top_idx)) { top = k; top_idx = i; }
-  }
-  if (lane == 0) { wave_key[wave] = top; wave_idx[wave] = top_idx; }
-  __syncthreads();
-  for (int w = 0; w < kWaves; ++w)
-    if (wave_key[w] > top || (wave_key[w] == top && wave_idx[w] < top_idx)) { top = wave_key[w]; top_idx = wave_idx[w]; }
-  if (top <= kKeyNone || s.greedy) {                   // (nothing to draw; or nothing else than the largest)
-    if (tid == 0) {
-      const bool none = top <= kKeyNone;
-      a.token[row] = none ? -1 : top_idx;
-      if (a.logprob != nullptr) a.logprob[row] = none ? -INFINITY : 0.f;
-      if (a.n_kept != nullptr) a.n_kept[row] = none ? 0 : 1;
-    }
-    return;
-  }
+__device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const RowSettings& s, uint32_t top, RowShared& sh) {
+  unsigned *count = sh.count, *wave_ties = sh.wave_ties, *wave_kept = sh.wave_kept;
+  unsigned long long *mass = sh.mass, *wave_mass = sh.wave_mass;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = a.vocab;
 
   // ---- radix descent: the cut behind the rank at which the count reaches `want` or the weights in front reach `target`
   unsigned long long set_mass = 0;                     // weights above the cut, its kept ties included
@@ -144,12 +157,12 @@ __global__ __launch_bounds__(64 * kWaves) void sample_row_kernel(SampleArgs a) {
           m += mass[at];
         }
         if (at < 0) { at = last; c -= count[at]; m -= mass[at]; }          // (fewer than wanted: all of them)
-        found_digit = at; found_count = c; found_mass = m;
+        sh.found_digit = at; sh.found_count = c; sh.found_mass = m;
       }
       __syncthreads();
-      prefix = (prefix << 8) | found_digit;
-      above = found_count;
-      above_mass = found_mass;
+      prefix = (prefix << 8) | sh.found_digit;
+      above = sh.found_count;
+      above_mass = sh.found_mass;
       __syncthreads();
     }
     const unsigned equal = count[prefix & 255];
@@ -202,16 +215,6 @@ __global__ __launch_bounds__(64 * kWaves) void sample_row_kernel(SampleArgs a) {
     total += wave_mass[w] + each * t;
     ties_before += wave_ties[w];
   }
-  // (the largest logit with min_p above 1: it alone)
-  const bool alone = s.min_p > 1.0;
-  if (alone) {
-    if (tid == 0) {
-      a.token[row] = top_idx;
-      if (a.logprob != nullptr) a.logprob[row] = 0.f;
-      if (a.n_kept != nullptr) a.n_kept[row] = 1;
-    }
-    return;
-  }
   const double target = s.u * static_cast<double>(total);
   unsigned long long before = 0;
   unsigned tb = 0;
@@ -252,18 +255,515 @@ __global__ __launch_bounds__(64 * kWaves) void sample_row_kernel(SampleArgs a) {
   }
 }
 
+// ---- a row in parts ------------------------------------------------------------------------------
+constexpr int kBins = 1024, kMaxParts = 64, kList = 4096;
+
+struct SamplePlan {
+  int parts, part_len, tile_len;      // a part is read by a workgroup, a tile (a quarter of it) by one of its wavefronts; parts 0: the list holds a row
+};
+struct Part {
+  uint32_t top, low;                  // largest and smallest finite logit's key (low 0xffffffff: none)
+  int top_idx, unused;
+};
+struct RowScratch {
+  Part part[kMaxParts];
+  unsigned long long mass[kBins];
+  unsigned long long tile_mass[4 * kMaxParts];
+  uint2 list[kList];                  // key, index
+  unsigned count[kBins];
+  unsigned tile_kept[4 * kMaxParts];
+  unsigned n_list, unused[3];
+};
+
+// The row as pieces of 16 bytes at aligned addresses: element e of them is logit e - shift.
+template <typename T>
+struct RowReader {
+  static constexpr int kPer = 16 / sizeof(T);
+  const T* row;
+  int shift, vocab;
+  __device__ __forceinline__ RowReader(const SampleArgs& a, int r) {
+    row = static_cast<const T*>(a.logits) + static_cast<size_t>(r) * a.stride;
+    shift = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    vocab = a.vocab;
+  }
+  // keys of the elements e .. e + kPer (e a multiple of kPer); what is not of the row gives kKeyNone and is not read
+  __device__ __forceinline__ void keys(int e, uint32_t (&k)[kPer]) const {
+    const int i = e - shift;
+    if (i >= 0 && i + kPer <= vocab) {
+      T v[kPer];
+      *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(row + i);
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) k[j] = logit_key(to_float(v[j]));
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) k[j] = i + j >= 0 && i + j < vocab ? logit_key(to_float(row[i + j])) : kKeyNone;
+    }
+  }
+};
+
+// The row's extremes from its parts: every wavefront for itself.
+__device__ __forceinline__ Part row_extremes(const RowScratch& ws, int parts) {
+  const int lane = threadIdx.x & 63;
+  Part p{0, 0xffffffffu, 0x7fffffff, 0};
+  if (lane < parts) p = ws.part[lane];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const uint32_t top = __shfl_xor(p.top, o, 64), low = __shfl_xor(p.low, o, 64);
+    const int idx = __shfl_xor(p.top_idx, o, 64);
+    if (top > p.top || (top == p.top && idx < p.top_idx)) { p.top = top; p.top_idx = idx; }
+    p.low = min(p.low, low);
+  }
+  return p;
+}
+
+// Bins of equal width from the largest logit (bin 0) down.  Rounded subtractions and products keep the order of the logits, so
+// the bins are in that order and equal logits share one.
+struct Bins {
+  float top, per;
+  bool usable;                        // not beside +inf
+  __device__ __forceinline__ Bins(uint32_t top_key, uint32_t low_key, double inv_t) {
+    top = logit_of(top_key);
+    const float span = fminf(top - logit_of(low_key), static_cast<float>(46.0 / inv_t));
+    per = span > 0.f ? kBins / span : 0.f;
+    usable = top_key != kKeyInf && span < INFINITY && per < INFINITY;
+  }
+  __device__ __forceinline__ int of(uint32_t key) const { return static_cast<int>(fminf((top - logit_of(key)) * per, static_cast<float>(kBins - 1))); }
+};
+
+struct Cuts {
+  int p_lo, p_hi, k_bin;              // candidates: bins p_lo .. p_hi, and k_bin; bins in front of p_lo are kept whole
+  unsigned count_lo, count_hi;        // tokens in front of p_lo, behind p_hi
+  unsigned count_k;                   // tokens in front of k_bin
+  unsigned listed;                    // candidates
+  unsigned long long mass_lo, mass_k, mass_all;      // weights in front of p_lo, of k_bin, of all bins
+};
+
+// Where the cuts fall, from the histogram.  With both top-k and top-p the weight that top-p refers to is known to the bin that top-k's cut
+// falls into, so top-p's has a first and a last possible bin.
+template <int N>
+__device__ __forceinline__ Cuts find_cuts(const RowScratch& ws, const RowSettings& s, int vocab) {
+  constexpr int kOwn = kBins / N;     // bins of a thread
+  __shared__ unsigned long long wave_mass[N / 64];
+  __shared__ unsigned wave_count[N / 64];
+  __shared__ Cuts cuts;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  unsigned c[kOwn], count = 0;
+  unsigned long long m[kOwn], mass = 0;
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    c[i] = ws.count[tid * kOwn + i];
+    m[i] = ws.mass[tid * kOwn + i];
+    count += c[i];
+    mass += m[i];
+  }
+  unsigned count_in = count;
+  unsigned long long mass_in = mass;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned cu = __shfl_up(count_in, o, 64);
+    const unsigned long long mu = __shfl_up(mass_in, o, 64);
+    if (lane >= o) { count_in += cu; mass_in += mu; }
+  }
+  if (lane == 63) { wave_count[wave] = count_in; wave_mass[wave] = mass_in; }
+  __syncthreads();
+  unsigned count_all = 0, count0 = count_in - count;
+  unsigned long long mass_all = 0, mass0 = mass_in - mass;
+  for (int w = 0; w < N / 64; ++w) {
+    if (w < wave) { count0 += wave_count[w]; mass0 += wave_mass[w]; }
+    count_all += wave_count[w];
+    mass_all += wave_mass[w];
+  }
+  const bool by_k = static_cast<unsigned>(s.top_k) < count_all, by_p = s.top_p < 1.0;
+  if (tid == 0) cuts = Cuts{kBins, kBins, kBins, count_all, count_all, count_all, 0, mass_all, mass_all, mass_all};
+  __syncthreads();
+  // (f(bin, tokens in front, weights in front, with the bin's own) for this thread's bins)
+  auto each = [&](auto&& f) __attribute__((always_inline)) {
+    unsigned cb = count0;
+    unsigned long long mb = mass0;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      f(tid * kOwn + i, cb, mb, cb + c[i], mb + m[i]);
+      cb += c[i];
+      mb += m[i];
+    }
+  };
+  __shared__ unsigned long long mass_with_k;
+  __shared__ unsigned count_with_k;
+  if (tid == 0) { mass_with_k = mass_all; count_with_k = count_all; }
+  __syncthreads();
+  if (by_k)
+    each([&](int b, unsigned cb, unsigned long long mb, unsigned ce, unsigned long long me) {
+      if (cb < static_cast<unsigned>(s.top_k) && static_cast<unsigned>(s.top_k) <= ce) {
+        cuts.k_bin = b; cuts.count_k = cb; cuts.mass_k = mb;
+        mass_with_k = me; count_with_k = ce;
+        if (!by_p) { cuts.p_lo = cuts.p_hi = b; cuts.count_lo = cb; cuts.count_hi = ce; cuts.mass_lo = mb; }
+      }
+    });
+  __syncthreads();
+  if (by_p) {
+    const double lo = s.top_p * static_cast<double>(cuts.mass_k), hi = s.top_p * static_cast<double>(mass_with_k);
+    each([&](int b, unsigned cb, unsigned long long mb, unsigned ce, unsigned long long me) {
+      if (static_cast<double>(me) >= lo && (b == 0 || static_cast<double>(mb) < lo)) { cuts.p_lo = b; cuts.count_lo = cb; cuts.mass_lo = mb; }
+      if (static_cast<double>(me) >= hi && (b == 0 || static_cast<double>(mb) < hi)) { cuts.p_hi = b; cuts.count_hi = ce; }
+    });
+  }
+  __syncthreads();
+  Cuts out = cuts;
+  out.listed = out.count_hi - out.count_lo + (out.k_bin > out.p_hi ? count_with_k - out.count_k : 0u);
+  return out;
+}
+
+__device__ __forceinline__ bool needs_cut(const SampleArgs& a, const RowSettings& s) { return s.top_k < a.vocab || s.top_p < 1.0; }
+
+template <typename T>
+__global__ __launch_bounds__(256) void sample_max_kernel(SampleArgs a, SamplePlan plan, RowScratch* __restrict__ scratch) {
+  constexpr int kPer = RowReader<T>::kPer;
+  __shared__ Part wave_part[4];
+  const int part = blockIdx.x, row = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  RowScratch& ws = scratch[row];
+  const RowReader<T> in(a, row);
+  for (int b = part * 256 + tid; b < kBins; b += plan.parts * 256) { ws.count[b] = 0; ws.mass[b] = 0; }
+  if (part == 0 && tid == 0) ws.n_list = 0;
+  uint32_t top = 0, low = 0xffffffffu;
+  int at = 0x7fffffff;
+  const int e1 = min((part + 1) * plan.part_len, a.vocab + in.shift);
+#pragma unroll 4
+  for (int e = part * plan.part_len + tid * kPer; e < e1; e += 256 * kPer) {
+    uint32_t k[kPer];
+    in.keys(e, k);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      if (k[j] > top) { top = k[j]; at = e + j - in.shift; }
+      if (k[j] > kKeyNone) low = min(low, k[j]);
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const uint32_t t = __shfl_xor(top, o, 64);
+    const int i = __shfl_xor(at, o, 64);
+    if (t > top || (t == top && i < at)) { top = t; at = i; }
+    low = min(low, static_cast<uint32_t>(__shfl_xor(low, o, 64)));
+  }
+  if (lane == 0) wave_part[wave] = Part{top, low, at, 0};
+  __syncthreads();
+  if (tid == 0) {
+    Part p = wave_part[0];
+    for (int w = 1; w < 4; ++w) {
+      const Part o = wave_part[w];
+      if (o.top > p.top || (o.top == p.top && o.top_idx < p.top_idx)) { p.top = o.top; p.top_idx = o.top_idx; }
+      p.low = min(p.low, o.low);
+    }
+    ws.part[part] = p;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void sample_hist_kernel(SampleArgs a, SamplePlan plan, RowScratch* __restrict__ scratch) {
+  constexpr int kPer = RowReader<T>::kPer;
+  __shared__ unsigned count[kBins];
+  __shared__ unsigned long long mass[kBins];
+  const int part = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+  RowScratch& ws = scratch[row];
+  const RowSettings s = settings_of(a, row);
+  if (s.greedy || !needs_cut(a, s)) return;
+  const Part x = row_extremes(ws, plan.parts);
+  if (x.top <= kKeyNone) return;
+  const Bins bins(x.top, x.low, s.inv_t);
+  if (!bins.usable) return;
+  for (int b = tid; b < kBins; b += 256) { count[b] = 0; mass[b] = 0; }
+  __syncthreads();
+  const RowReader<T> in(a, row);
+  const bool weigh = s.top_p < 1.0;
+  const int e1 = min((part + 1) * plan.part_len, a.vocab + in.shift);
+  for (int e = part * plan.part_len + tid * kPer; e < e1; e += 256 * kPer) {
+    uint32_t k[kPer];
+    in.keys(e, k);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (k[j] > kKeyNone) {
+        const int b = bins.of(k[j]);
+        atomicAdd(&count[b], 1u);
+        if (weigh) atomicAdd(&mass[b], fixed_of(weight_of(k[j], x.top, s.inv_t), a.shift));
+      }
+  }
+  __syncthreads();
+  for (int b = tid; b < kBins; b += 256)
+    if (count[b] != 0) {
+      atomicAdd(&ws.count[b], count[b]);
+      if (mass[b] != 0) atomicAdd(&ws.mass[b], mass[b]);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void sample_tiles_kernel(SampleArgs a, SamplePlan plan, RowScratch* __restrict__ scratch) {
+  constexpr int kPer = RowReader<T>::kPer;
+  const int part = blockIdx.x, row = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  RowScratch& ws = scratch[row];
+  const RowSettings s = settings_of(a, row);
+  if (s.greedy) return;
+  const Part x = row_extremes(ws, plan.parts);
+  if (x.top <= kKeyNone) return;
+  const Bins bins(x.top, x.low, s.inv_t);
+  const bool cut = needs_cut(a, s);
+  if (cut && !bins.usable) return;
+  int p_lo = kBins, p_hi = kBins, k_bin = kBins;
+  if (cut) {
+    const Cuts c = find_cuts<256>(ws, s, a.vocab);
+    if (c.listed > kList) return;                      // (the last kernel does the row alone)
+    p_lo = c.p_lo; p_hi = c.p_hi; k_bin = c.k_bin;
+  }
+  const RowReader<T> in(a, row);
+  const int tile = part * 4 + wave, e1 = min((tile + 1) * plan.tile_len, a.vocab + in.shift);
+  unsigned kept = 0;
+  unsigned long long sum = 0;
+  for (int e = tile * plan.tile_len + lane * kPer; e < e1; e += 64 * kPer) {
+    uint32_t k[kPer];
+    in.keys(e, k);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (k[j] > kKeyNone) {
+        const int b = cut ? bins.of(k[j]) : -1;
+        if (b < p_lo) {
+          const double w = weight_of(k[j], x.top, s.inv_t);
+          if (w >= s.min_p) { ++kept; sum += fixed_of(w, a.shift); }
+        } else if (b <= p_hi || b == k_bin) {
+          const unsigned at = atomicAdd(&ws.n_list, 1u);
+          if (at < kList) ws.list[at] = make_uint2(k[j], e + j - in.shift);
+        }
+      }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) { kept += __shfl_xor(kept, o, 64); sum += __shfl_xor(sum, o, 64); }
+  if (lane == 0) { ws.tile_kept[tile] = kept; ws.tile_mass[tile] = sum; }
+}
+
+template <int N, typename V>
+__device__ __forceinline__ V block_sum(V v, V* part) {               // over the workgroup's 64 N threads
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  V all = 0;
+  for (int w = 0; w < N; ++w) all += part[w];
+  return all;
+}
+template <int N>
+__device__ __forceinline__ unsigned long long block_before(unsigned long long v, unsigned long long* part) {     // sum of the threads in front
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  unsigned long long in = v;
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned long long up = __shfl_up(in, o, 64);
+    if (lane >= o) in += up;
+  }
+  __syncthreads();
+  if (lane == 63) part[wave] = in;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) in += part[w];
+  return in - v;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a, SamplePlan plan, RowScratch* __restrict__ scratch) {
+  union Shared {
+    RowShared row;
+    struct { unsigned long long order[kList]; unsigned long long tile[4 * kMaxParts]; } list;
+  };
+  __shared__ Shared sh;
+  __shared__ unsigned long long part_mass[kWaves], found_before;
+  __shared__ unsigned part_count[kWaves];
+  __shared__ int found;
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const RowSettings s = settings_of(a, row);
+  const bool parts = plan.parts > 0, cut = !parts || needs_cut(a, s);
+  const RowReader<T> in(a, row);
+  const int tile_len = parts ? plan.tile_len : kList, shift = parts ? in.shift : 0, n_tiles = parts ? 4 * plan.parts : 1;
+  uint32_t top;
+  int top_idx;
+  Part x{0, 0, 0, 0};
+  Cuts c{0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+  int n_list = 0;
+  bool whole = false;                                  // the list does not hold the candidates
+  if (parts) {
+    x = row_extremes(scratch[row], plan.parts);
+    top = x.top;
+    top_idx = x.top_idx;
+  } else {
+    // the whole row is the list: (key, ~index), nothing behind it
+    unsigned mine = 0;
+    for (int i = tid; i < a.vocab; i += kThreads) {
+      const uint32_t k = key_at<T>(a, row, i);
+      sh.list.order[i] = k > kKeyNone ? (static_cast<unsigned long long>(k) << 32) | ~static_cast<uint32_t>(i) : 0ull;
+      mine += k > kKeyNone;
+    }
+    n_list = a.vocab;
+    const unsigned finite = block_sum<kWaves>(mine, part_count);
+    c.count_hi = finite;
+    uint32_t hi = 0;
+    int at = 0x7fffffff;
+    for (int i = tid; i < a.vocab; i += kThreads) {
+      const uint32_t k = static_cast<uint32_t>(sh.list.order[i] >> 32);
+      if (k > hi) { hi = k; at = i; }
+    }
+    unsigned long long best = hi == 0 ? 0ull : (static_cast<unsigned long long>(hi) << 32) | ~static_cast<uint32_t>(at);
+    for (int o = 32; o > 0; o >>= 1) best = max(best, __shfl_xor(best, o, 64));
+    __syncthreads();
+    if (lane == 0) part_mass[tid >> 6] = best;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) best = max(best, part_mass[w]);
+    top = static_cast<uint32_t>(best >> 32);
+    top_idx = static_cast<int>(~static_cast<uint32_t>(best));
+    __syncthreads();
+  }
+  if (top <= kKeyNone || s.greedy) {                   // (nothing to draw; or nothing else than the largest)
+    if (tid == 0) {
+      const bool none = top <= kKeyNone;
+      a.token[row] = none ? -1 : top_idx;
+      if (a.logprob != nullptr) a.logprob[row] = none ? -INFINITY : 0.f;
+      if (a.n_kept != nullptr) a.n_kept[row] = none ? 0 : 1;
+    }
+    return;
+  }
+  const Bins bins(top, parts ? x.low : top, s.inv_t);
+  if (parts && cut) {
+    whole = !bins.usable;
+    if (!whole) {
+      c = find_cuts<kThreads>(scratch[row], s, a.vocab);
+      whole = c.listed > kList;
+      n_list = static_cast<int>(c.listed);
+    }
+    if (whole) {
+      sample_row<T>(a, row, s, top, sh.row);
+      return;
+    }
+    for (int i = tid; i < n_list; i += kThreads) {
+      const uint2 v = scratch[row].list[i];
+      sh.list.order[i] = (static_cast<unsigned long long>(v.x) << 32) | ~v.y;
+    }
+  }
+  // ---- the candidates in order: largest logit, then lowest index
+  int n_pow = 1;
+  while (n_pow < n_list) n_pow <<= 1;
+  for (int i = n_list + tid; i < n_pow; i += kThreads) sh.list.order[i] = 0ull;
+  for (int i = tid; i < n_tiles; i += kThreads) sh.list.tile[i] = parts ? scratch[row].tile_mass[i] : 0ull;
+  __syncthreads();
+  for (int len = 2; len <= n_pow; len <<= 1)
+    for (int half = len >> 1; half > 0; half >>= 1) {
+      for (int i = tid; i < n_pow / 2; i += kThreads) {
+        const int lo = (i / half) * 2 * half + i % half, hi = lo + half;
+        const unsigned long long u = sh.list.order[lo], v = sh.list.order[hi];
+        if ((u < v) == ((lo & len) == 0)) { sh.list.order[lo] = v; sh.list.order[hi] = u; }
+      }
+      __syncthreads();
+    }
+  // ---- the cut among them.  This thread's are own .. own + per
+  const int per = max(1, n_pow / kThreads), own = tid * per;
+  auto weight_at = [&](int i) { return weight_of(static_cast<uint32_t>(sh.list.order[i] >> 32), top, s.inv_t); };
+  int n_cand = n_list, kept_list = 0;
+  if (!parts) n_cand = static_cast<int>(c.count_hi);
+  if (cut) {
+    const bool by_k = parts ? c.k_bin < kBins : s.top_k < n_cand;
+    // tokens that pass top-k: the list's first n_k.  (Candidates of p_lo .. p_hi come first; k_bin is among or behind them.)
+    const int base_k = !parts ? 0 : c.k_bin <= c.p_hi ? static_cast<int>(c.count_k - c.count_lo) : static_cast<int>(c.count_hi - c.count_lo);
+    const int n_k = by_k ? base_k + s.top_k - static_cast<int>(c.count_k) : n_cand;
+    unsigned long long in_k = 0, mine = 0;
+    for (int i = own; i < min(own + per, n_cand); ++i) {
+      const unsigned long long w = fixed_of(weight_at(i), a.shift);
+      mine += w;
+      if (i >= base_k && i < n_k) in_k += w;
+    }
+    unsigned long long mass_k = 0;
+    if (s.top_p < 1.0) {
+      mass_k = block_sum<kWaves>(in_k, part_mass);
+      mass_k = parts && !by_k ? c.mass_all : c.mass_k + mass_k;
+    }
+    unsigned long long before = c.mass_lo + block_before<kWaves>(mine, part_mass);
+    const double target = s.top_p * static_cast<double>(mass_k);
+    unsigned kept = 0;
+    for (int i = own; i < min(own + per, n_cand); ++i) {
+      const double w = weight_at(i);
+      const unsigned long long f = fixed_of(w, a.shift);
+      const bool first = i == 0 && c.p_lo == 0;        // rank 0
+      if (first || (i < n_k && (s.top_p >= 1.0 || static_cast<double>(before) < target) && w >= s.min_p)) {
+        ++kept;
+        const int e = static_cast<int>(~static_cast<uint32_t>(sh.list.order[i])) + shift;
+        atomicAdd(&sh.list.tile[e / tile_len], f);
+      }
+      before += f;
+    }
+    kept_list = static_cast<int>(block_sum<kWaves>(kept, part_count));
+  }
+  const unsigned long long last = kept_list > 0 ? sh.list.order[kept_list - 1] : ~0ull;     // (key, ~index) of the last kept candidate
+  __syncthreads();
+  // ---- the tile the number falls into
+  const unsigned long long here = tid < n_tiles ? sh.list.tile[tid] : 0ull;
+  const unsigned long long front = block_before<kWaves>(here, part_mass), total = block_sum<kWaves>(here, part_mass);
+  const unsigned n_kept = block_sum<kWaves>(parts && tid < n_tiles ? scratch[row].tile_kept[tid] : 0u, part_count) + kept_list;
+  const double target = s.u * static_cast<double>(total);
+  if (static_cast<double>(front) <= target && static_cast<double>(front + here) > target) { found = tid; found_before = front; }
+  __syncthreads();
+  const int share = (tile_len + kThreads - 1) / kThreads, e0 = found * tile_len + tid * share, e1 = min(min(e0 + share, (found + 1) * tile_len), a.vocab + shift);
+  auto kept_weight = [&](int e) {
+    const int i = e - shift;
+    if (i < 0) return 0.0;
+    const uint32_t k = key_at<T>(a, row, i);
+    if (k <= kKeyNone) return 0.0;
+    if (cut && !(parts && bins.of(k) < c.p_lo) && ((static_cast<unsigned long long>(k) << 32) | ~static_cast<uint32_t>(i)) < last) return 0.0;
+    const double w = weight_of(k, top, s.inv_t);
+    return w >= s.min_p ? w : 0.0;
+  };
+  unsigned long long sum = 0;
+  for (int e = e0; e < e1; ++e) sum += fixed_of(kept_weight(e), a.shift);
+  unsigned long long before = found_before + block_before<kWaves>(sum, part_mass);
+  if (static_cast<double>(before) <= target && static_cast<double>(before + sum) > target)
+    for (int e = e0; e < e1; ++e) {
+      const double w = kept_weight(e);
+      before += fixed_of(w, a.shift);
+      if (static_cast<double>(before) > target) {
+        a.token[row] = e - shift;
+        if (a.logprob != nullptr) a.logprob[row] = static_cast<float>(log(w / ldexp(static_cast<double>(total), -a.shift)));
+        if (a.n_kept != nullptr) a.n_kept[row] = static_cast<int>(n_kept);
+        break;
+      }
+    }
+}
+
+// Parts of at least 2048 logits, so many that a call has about a thousand workgroups (four on a compute unit), at most 64 a row.
+SamplePlan sample_plan(int n_rows, int vocab) {
+  SamplePlan p{0, 0, 0};
+  if (vocab <= kList) return p;
+  const long long wanted = std::max(1, std::min(kMaxParts, 1024 / std::max(1, n_rows)));
+  const long long len = std::max((vocab + 8 + wanted - 1) / wanted, 2048ll);      // (8: a row's beginning inside a piece)
+  p.part_len = static_cast<int>((len + 2047) / 2048 * 2048);
+  p.tile_len = p.part_len / 4;
+  p.parts = (vocab + 8 + p.part_len - 1) / p.part_len;
+  return p;
+}
+
 }  // namespace
 
-size_t sample_bytes(int, int) { return 0; }
+size_t sample_bytes(int n_rows, int vocab) { return sample_plan(n_rows, vocab).parts > 0 ? static_cast<size_t>(n_rows) * sizeof(RowScratch) : 0; }
+
+template <typename T>
+static void launch_sample_t(const SampleArgs& a, const SamplePlan& plan, RowScratch* ws, hipStream_t stream) {
+  const dim3 grid(plan.parts, a.n_rows);
+  if (plan.parts > 0) {
+    hipLaunchKernelGGL(sample_max_kernel<T>, grid, dim3(256), 0, stream, a, plan, ws);
+    if (a.top_k != nullptr || a.top_p != nullptr) hipLaunchKernelGGL(sample_hist_kernel<T>, grid, dim3(256), 0, stream, a, plan, ws);
+    hipLaunchKernelGGL(sample_tiles_kernel<T>, grid, dim3(256), 0, stream, a, plan, ws);
+  }
+  hipLaunchKernelGGL(sample_draw_kernel<T>, dim3(a.n_rows), dim3(kThreads), 0, stream, a, plan, ws);
+}
 
 void launch_sample(const void* logits, int logits_dtype, int n_rows, int vocab, long long stride, const float* temperature,
                    const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* token, float* logprob,
                    int32_t* n_kept, void* workspace, hipStream_t stream) {
   int bits = 0;
   while ((1ll << bits) < vocab) ++bits;
-  const SampleArgs a{logits, n_rows, vocab, stride, temperature, top_k, top_p, min_p, u, token, logprob, n_kept, 62 - bits};
-  if (logits_dtype == CC_BF16) hipLaunchKernelGGL(sample_row_kernel<bf16_t>, dim3(n_rows), dim3(64 * kWaves), 0, stream, a);
-  else hipLaunchKernelGGL(sample_row_kernel<float>, dim3(n_rows), dim3(64 * kWaves), 0, stream, a);
+  const SampleArgs a{logits, n_rows, vocab, stride, temperature, top_k, top_p, min_p, u, token, logprob, n_kept, std::min(50, 62 - bits)};
+  const SamplePlan plan = sample_plan(n_rows, vocab);
+  RowScratch* ws = static_cast<RowScratch*>(workspace);
+  if (logits_dtype == CC_BF16) launch_sample_t<bf16_t>(a, plan, ws, stream);
+  else launch_sample_t<float>(a, plan, ws, stream);
 }
 
 }  // namespace cc
