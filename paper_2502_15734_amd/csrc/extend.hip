@@ -89,27 +89,36 @@ __global__ __launch_bounds__(256) void extend_need_kernel(ExtendArgs a, Need* __
   need[r] = Need{static_cast<int>(pages), static_cast<int>(rows), status, static_cast<int>(tokens)};
 }
 
-// Inclusive scan over the workgroup's 64 W threads, of N sums at once.  Sums of what is wanted stop at 2^32 - 1 (beyond any limit).
+// Sums of what is wanted stop at 2^32 - 1 (beyond any limit).
 __device__ __forceinline__ unsigned add_up(unsigned x, unsigned y) { return __builtin_elementwise_add_sat(x, y); }
-template <int N, int W>
-__device__ __forceinline__ void block_scan(unsigned (&v)[N], unsigned (*part)[N]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+
+// Inclusive scan over the workgroup's 64 W threads, of N sums at once.  STOP: sums stop at 2^32 - 1, otherwise they are mod 2^32.
+template <bool STOP, int N, int W>
+__device__ __forceinline__ void block_scan(unsigned (&v)[N], unsigned (*part)[N], unsigned (&all)[N]) {      // all: the totals
+  auto add = [](unsigned x, unsigned y) { return STOP ? add_up(x, y) : x + y; };
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const unsigned up = __shfl_up(v[i], o, 64);
-      if (lane >= o) v[i] = add_up(v[i], up);
+      if (lane >= o) v[i] = add(v[i], up);
     }
   if (lane == 63)
 #pragma unroll
     for (int i = 0; i < N; ++i) part[wave][i] = v[i];
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < W; ++w)
-    if (w < wave)
+  for (int i = 0; i < N; ++i) {                        // (lane w of each wavefront takes the sum of wavefront w)
+    unsigned sum = lane < W ? part[lane][i] : 0u;
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = add_up(v[i], part[w][i]);
+    for (int o = 1; o < W; o <<= 1) {
+      const unsigned up = __shfl_up(sum, o, 64);
+      if (lane >= o) sum = add(sum, up);
+    }
+    all[i] = __builtin_amdgcn_readlane(sum, W - 1);
+    if (wave > 0) v[i] = add(v[i], __builtin_amdgcn_readlane(sum, max(wave - 1, 0)));
+  }
 }
 
 // Sums over the requests in front: their wishes, and what they get.
@@ -122,23 +131,22 @@ template <int W>
 __device__ __forceinline__ Place place_round(const ExtendArgs& a, Need n, bool here, Running& run, Need* decided) {
   __shared__ unsigned part2[W][2], part4[W][4];
   unsigned w[2] = {static_cast<unsigned>(n.pages), static_cast<unsigned>(n.rows)};
-  block_scan<2, W>(w, part2);
+  unsigned all_w[2], all_g[4];
+  block_scan<true, 2, W>(w, part2, all_w);
   if (n.rows > 0 && add_up(run.rows_wanted, w[1]) > static_cast<unsigned>(a.max_rows)) n.status = CC_EXTEND_NO_ROWS;
   if (n.pages > 0 && add_up(run.pages_wanted, w[0]) > static_cast<unsigned>(a.n_free)) n.status = CC_EXTEND_NO_PAGES;
   const bool ok = n.status == CC_EXTEND_OK;
   if (!ok) n.pages = n.rows = 0;
   unsigned g[4] = {static_cast<unsigned>(n.pages), static_cast<unsigned>(n.rows), static_cast<unsigned>(n.old_tokens) + n.rows, here && !ok};
-  block_scan<4, W>(g, part4);
+  block_scan<false, 4, W>(g, part4, all_g);
   const Place p{static_cast<int>(run.pages + g[0]) - n.pages, static_cast<int>(run.rows + g[1]) - n.rows,
                 static_cast<int>(run.tokens + g[2]) - n.old_tokens - n.rows, ok};
-  for (int k = 0; k < W; ++k) {
-    run.pages_wanted = add_up(run.pages_wanted, part2[k][0]);
-    run.rows_wanted = add_up(run.rows_wanted, part2[k][1]);
-    run.pages += part4[k][0];
-    run.rows += part4[k][1];
-    run.tokens += part4[k][2];
-    run.refused += part4[k][3];
-  }
+  run.pages_wanted = add_up(run.pages_wanted, all_w[0]);
+  run.rows_wanted = add_up(run.rows_wanted, all_w[1]);
+  run.pages += all_g[0];
+  run.rows += all_g[1];
+  run.tokens += all_g[2];
+  run.refused += all_g[3];
   __syncthreads();
   *decided = n;
   return p;
@@ -326,21 +334,10 @@ __global__ __launch_bounds__(64 * W) void extend_small_kernel(ExtendArgs a) {
     if (r < a.n_requests) { sh.flags[r] = 0; sh.tokens[r] = 0; }
   }
   for (int j = tid; j < kSmallRows / 2; j += kThreads) reinterpret_cast<unsigned*>(sh.row_seg)[j] = 0;
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    in[i] = v[i];
-    for (int o = 1; o < 64; o <<= 1) {
-      const unsigned up = __shfl_up(in[i], o, 64);
-      if (lane >= o) in[i] += up;
-    }
-    if (lane == 63) wave_sum[wave][i] = in[i];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    for (int w = 0; w < wave; ++w) in[i] += wave_sum[w][i];
-    in[i] -= v[i];
-  }
+  unsigned all[3];
+  for (int i = 0; i < 3; ++i) in[i] = v[i];
+  block_scan<false, 3, W>(in, wave_sum, all);
+  for (int i = 0; i < 3; ++i) in[i] -= v[i];
 #pragma unroll
   for (int i = 0; i < kOwn; ++i) {
     const int s = tid * kOwn + i;
