@@ -14,6 +14,7 @@
 //
 // The softmax reference of a column is shared by the four lane groups and moves only when a logit is more than kSlack above it.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_util.h"
 
@@ -21,6 +22,12 @@ namespace cc {
 
 namespace {
 
+#ifndef CC_T1
+#define CC_T1 512
+#endif
+#ifndef CC_T2
+#define CC_T2 512
+#endif
 constexpr float kSlack = 8.f;         // in powers of two
 constexpr int kWindow = 256;          // pages listed in LDS at a time
 constexpr float kLog2e = 1.4426950408889634f;
@@ -36,8 +43,8 @@ struct AppendArgs {
   float* lse;
   ValueSource vs;
   int n_requests, n_blocks, hq, hkv;
-  // division of the keys
-  int n_splits, split_pages;
+  // division of the work
+  int n_splits, split_pages, col_groups;
   float *part_o, *part_ml;            // [row][head][split][D], [row][head][split][2]
   int32_t* row_splits;                // [row] ranges its request has (1: the output is written)
 };
@@ -50,7 +57,7 @@ __device__ __forceinline__ int pages_of(int tokens) { return (max(tokens, 0) + k
 
 // Pages [first, first + kWindow) of a request into list[] (thread i: page first + i), those behind its last one with n_valid 0;
 // returns the number of pages the request has.  Thread i also takes segment i of 256 at a time, whose page counts are scanned.
-__device__ __forceinline__ int list_pages(const AppendArgs& a, int s_begin, int s_end, int first, int p_max, Page* list, int4* segs, int* seg_end,
+__device__ __forceinline__ int list_pages(const AppendArgs& a, int s_begin, int s_end, int first, Page* list, int4* segs, int* seg_end,
                                           int* wave_pages) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, want = first + tid;
   Page page{0, 0, 0, 0};
@@ -85,7 +92,7 @@ __device__ __forceinline__ int list_pages(const AppendArgs& a, int s_begin, int 
       const int4 sg = segs[lo];
       const int nth = want - (seg_end[lo] - pages_of(sg.y)), blk = a.block_tab[sg.z + nth];
       page.pos0 = sg.x + nth * kBlock;
-      if (blk >= 0 && blk < a.n_blocks && page.pos0 <= p_max) {
+      if (blk >= 0 && blk < a.n_blocks) {
         page.blk = page.value = blk;
         page.n_valid = min(sg.y - nth * kBlock, kBlock);
         if (a.vs.v_map != nullptr) {
@@ -180,16 +187,45 @@ template <int D> struct Tile<float, D> {
   static __device__ __forceinline__ Piece piece(const float (&x)[4]) { return Piece{x[0], x[1], x[2], x[3]}; }
 };
 
+// What a workgroup does.  Workgroups go to the eight XCDs in turn; the column groups of one range of keys, which read the same pages, follow
+// each other on one XCD, whose L2 then has them.
+struct Unit {
+  int split, kvh, req, col_group;     // req: n_requests and more: nothing
+};
+__device__ __forceinline__ Unit unit_of(const AppendArgs& a) {
+  const unsigned at = blockIdx.x / 8, u = blockIdx.x % 8 + 8 * (at / a.col_groups), rest = u / a.n_splits;
+  return Unit{static_cast<int>(u % a.n_splits), static_cast<int>(rest % a.hkv), static_cast<int>(rest / a.hkv), static_cast<int>(at % a.col_groups)};
+}
+// where the result of a range goes: the parts, or the output if the request has no other
+template <typename T, int D>
+__device__ __forceinline__ void store_result(const AppendArgs& a, size_t at, int split, int n_splits, int d, const f32x4& v, float top, float sum) {
+  if (n_splits == 1) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;                 // (no key: zeros, and -inf for the logarithm)
+    T o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = from_float<T>(v[e] * inv);
+    T* op = static_cast<T*>(a.out) + at * D + d;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(op) = *reinterpret_cast<const uint2*>(o);
+    else *reinterpret_cast<uint4*>(op) = *reinterpret_cast<const uint4*>(o);
+    if (d == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : top / kLog2e + logf(sum);
+  } else {
+    *reinterpret_cast<f32x4*>(a.part_o + (at * a.n_splits + split) * D + d) = v;
+    if (d == 0) *reinterpret_cast<float2*>(a.part_ml + (at * a.n_splits + split) * 2) = make_float2(top, sum);
+  }
+}
+
 // One (range of pages, KV head and 16 NC columns, request).  Column c is head c % G of the request's row c / G.
 template <typename T, int D, int NC>
-__global__ __launch_bounds__(256, NC == 4 ? 1 : 2) void append_split_kernel(AppendArgs a, InvFreq inv_freq) {
+__global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvFreq inv_freq) {
   typedef Tile<T, D> Keys;
   typedef typename Keys::Piece Piece;
   constexpr int kTok = Keys::kTok, kPer = 16 / sizeof(T), kQ = D / 4 / kPer;      // elements of a piece; pieces of a query a lane holds
   constexpr int kRow = D + 4;                                                    // (a column of the outputs in LDS: banks apart)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-  const int r = blockIdx.z, kvh = blockIdx.y, split = blockIdx.x % a.n_splits, group = a.hq / a.hkv;
-  const int col0 = blockIdx.x / a.n_splits * 16 * NC, row0 = a.cu_q[r], n_cols = (a.cu_q[r + 1] - row0) * group;
+  const Unit unit = unit_of(a);
+  const int r = unit.req, kvh = unit.kvh, split = unit.split, group = a.hq / a.hkv;
+  if (r >= a.n_requests) return;
+  const int col0 = unit.col_group * 16 * NC, row0 = a.cu_q[r], n_cols = (a.cu_q[r + 1] - row0) * group;
   if (col0 >= n_cols) return;
   const int s_begin = a.req_seg_off[r], s_end = a.req_seg_off[r + 1];
 
@@ -228,7 +264,7 @@ __global__ __launch_bounds__(256, NC == 4 ? 1 : 2) void append_split_kernel(Appe
   }
 
   const int first_page = split * a.split_pages;
-  int n_pages = list_pages(a, s_begin, s_end, first_page, p_max, sh.in.list, sh.in.segs, sh.in.seg_end, sh.in.wave_pages);
+  int n_pages = list_pages(a, s_begin, s_end, first_page, sh.in.list, sh.in.segs, sh.in.seg_end, sh.in.wave_pages);
   if (first_page >= max(n_pages, 1)) return;                                        // (the same in all wavefronts)
   const int n_splits = min((max(n_pages, 1) + a.split_pages - 1) / a.split_pages, a.n_splits);
   const int end_page = split == a.n_splits - 1 ? n_pages : min(n_pages, first_page + a.split_pages);
@@ -336,7 +372,7 @@ __global__ __launch_bounds__(256, NC == 4 ? 1 : 2) void append_split_kernel(Appe
     at += kWindow;
     __syncthreads();
     if (at >= end_page) break;
-    list_pages(a, s_begin, s_end, at, p_max, sh.in.list, sh.in.segs, sh.in.seg_end, sh.in.wave_pages);
+    list_pages(a, s_begin, s_end, at, sh.in.list, sh.in.segs, sh.in.seg_end, sh.in.wave_pages);
   }
 
   // ---- the four wavefronts' sums, and the result of this range
@@ -362,25 +398,293 @@ __global__ __launch_bounds__(256, NC == 4 ? 1 : 2) void append_split_kernel(Appe
         }
         const int row = row0 + col / group;
         const size_t at = static_cast<size_t>(row) * a.hq + kvh * group + col % group;
-        if (n_splits == 1) {
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;           // (no key: zeros, and -inf for the logarithm)
-          T* op = static_cast<T*>(a.out) + at * D + d;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) op[e] = from_float<T>(v[e] * inv);
-          if (d == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : top / kLog2e + logf(sum);
-        } else {
-          *reinterpret_cast<f32x4*>(a.part_o + (at * a.n_splits + split) * D + d) = v;
-          if (d == 0) {
-            float* ml = a.part_ml + (at * a.n_splits + split) * 2;
-            ml[0] = top;
-            ml[1] = sum;
-          }
-        }
+        store_result<T, D>(a, at, split, n_splits, d, v, top, sum);
         if (split == 0 && d == 0 && kvh == 0 && col % group == 0) a.row_splits[row] = n_splits;
       }
     }
     __syncthreads();
   }
+}
+
+// ---- many columns -------------------------------------------------------------------------------
+// A draft to check or a further question: 33 columns and more (rows times heads of a group) share the keys.  Workgroup = 32 CW columns x a range
+// of pages; tiles of 64 keys go through LDS (registers hold the next tile, two images, one barrier per tile), so that a page is read
+// once for all its columns.  CW = 4: each wavefront multiplies its 32 columns with all 64 keys; CW = 2: two wavefronts per 32 columns take 32
+// keys each and meet at the end.  Bound by the matrix cores and the exponentials beside them from some hundred columns on.
+//
+// v_mfma_f32_32x32x16_bf16, S^T = K Q^T and O^T = V^T P^T with lane = (n = lane % 32, h = lane / 32), column n.  As above the key rows are
+// ordered so that a lane's logits are the tokens 8 h .. 8 h + 7 of each page: row 8 a + 4 b + c of a 32-key block is token
+// 8 b + 4 (a % 2) + c of page a / 2.  Image (16-byte pieces):
+//   K  token t of the tile, piece ch of its row:        t * D / 8 + (ch ^ f(t)),  f(t) = t % 4 + 4 (t / 8 % 2)
+//   V  page, dim d, half h of its row of 16 tokens:     8 D + page * 2 D + h * D + (d ^ 4 h)
+// (eight lanes of a read or write meet eight different 16-byte columns of the banks)
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+constexpr int kTileKeys = 64, kTilePages = kTileKeys / kBlock;
+
+template <int D, int CW>
+__global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFreq inv_freq) {
+  constexpr int KS = 4 / CW, kStage = D / 32, kImage = 16 * D;          // pieces a thread stages of K (and of V); pieces of an image
+  constexpr int kBlocks = 2 / KS;                                      // 32-key blocks of a tile that are this wavefront's
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+  const int cw = wave % CW, ks = wave / CW;
+  const Unit unit = unit_of(a);
+  const int r = unit.req, kvh = unit.kvh, split = unit.split, group = a.hq / a.hkv;
+  if (r >= a.n_requests) return;
+  const int row0 = a.cu_q[r], n_cols = (a.cu_q[r + 1] - row0) * group, wg_col = unit.col_group * 32 * CW;
+  if (wg_col >= n_cols) return;
+  const int s_begin = a.req_seg_off[r], s_end = a.req_seg_off[r + 1];
+
+  __shared__ u32x4 image[2 * kImage];
+  __shared__ Page list[kWindow];
+  __shared__ int odd[kWindow / kTilePages];
+  __shared__ int2 edge_pos[4];
+  struct Scratch { int4 segs[256]; int seg_end[256]; int wave_pages[4]; };
+  Scratch& scratch = *reinterpret_cast<Scratch*>(image);               // (while a list is made no image is in use)
+
+  const int col = wg_col + 32 * cw + n, my_col = min(col, n_cols - 1), row = row0 + my_col / group, pos = a.q_pos[row];
+  u32x4 raw[D / 16];
+  {
+    const int src = a.src_rows != nullptr ? a.src_rows[row] : row;
+    const bf16_t* qp = static_cast<const bf16_t*>(a.q) + (static_cast<size_t>(src) * a.hq + kvh * group + my_col % group) * D + 8 * h;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) raw[i] = *reinterpret_cast<const u32x4*>(qp + 16 * i);
+  }
+  const int first_page = split * a.split_pages;
+  const int n_pages = list_pages(a, s_begin, s_end, first_page, list, scratch.segs, scratch.seg_end, scratch.wave_pages);
+  if (first_page >= max(n_pages, 1)) return;
+  const int n_splits = min((max(n_pages, 1) + a.split_pages - 1) / a.split_pages, a.n_splits);
+  const int end_page = split == a.n_splits - 1 ? n_pages : min(n_pages, first_page + a.split_pages);
+  // positions of the wavefront's columns and of the workgroup's (columns behind the last repeat its row)
+  const int p_min = wave_min_i(pos), p_max = wave_max_i(pos);
+  if (lane == 0) edge_pos[wave] = make_int2(p_min, p_max);
+  __syncthreads();
+  const int p_first = min(min(edge_pos[0].x, edge_pos[1].x), min(edge_pos[2].x, edge_pos[3].x));
+  const int p_last = max(max(edge_pos[0].y, edge_pos[1].y), max(edge_pos[2].y, edge_pos[3].y));
+
+  const size_t block_elems = static_cast<size_t>(a.hkv) * kBlock * D, head_off = static_cast<size_t>(kvh) * kBlock * D;
+  const bf16_t *k_pool = static_cast<const bf16_t*>(a.k_pool) + head_off, *v_pool = static_cast<const bf16_t*>(a.v_pool) + head_off;
+  const bf16_t* v_shared = static_cast<const bf16_t*>(a.vs.v_shared) + head_off;
+  u32x4 kr[kStage], vr[kStage];
+  // the tile that begins at entry i of the list, `here` entries of which are this range's (a wavefront's pieces of one load lie in one page)
+  auto load = [&](int i, int here) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kStage; ++j) {
+      const int pg = (wave * 64 + 256 * j) / (2 * D), piece = (tid + 256 * j) % (2 * D);
+      const Page p = list[min(i + pg, kWindow - 1)];
+      const int blk = __builtin_amdgcn_readfirstlane(p.blk), value = __builtin_amdgcn_readfirstlane(p.value);
+      const int n_valid = i + pg >= here ? 0 : __builtin_amdgcn_readfirstlane(p.n_valid);
+      kr[j] = *reinterpret_cast<const u32x4*>(k_pool + blk * block_elems + piece * 8);
+      const bf16_t* from = value >= 0 ? v_pool + value * block_elems : v_shared + (-1 - value) * block_elems;
+      vr[j] = *reinterpret_cast<const u32x4*>(from + piece * 8);
+      if (n_valid < kBlock) {                                         // padding slots: zeros, or 0 x what lies there would be a product
+        auto keep = [&](int e) { const int t = 8 * (piece & 1) + 2 * e; return (t < n_valid ? 0xffffu : 0u) | (t + 1 < n_valid ? 0xffff0000u : 0u); };
+        vr[j] &= u32x4{keep(0), keep(1), keep(2), keep(3)};
+      }
+    }
+  };
+  // ... into image `buf`.  A tile with values that are not finite and that only some columns see is set aside (odd): 0 x such a value would reach
+  // the others.
+  auto store = [&](int buf, int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kStage; ++j) {
+      const int at = tid + 256 * j, pg = at / (2 * D), piece = at % (2 * D);
+      const int t = pg * kBlock + piece / (D / 8), ch = piece % (D / 8);
+      image[buf * kImage + t * (D / 8) + (ch ^ ((t & 3) | ((t >> 1) & 4)))] = kr[j];
+      const int d = piece >> 1, half = piece & 1;
+      image[buf * kImage + 8 * D + pg * 2 * D + half * D + (d ^ (4 * half))] = vr[j];
+      if (__builtin_amdgcn_readfirstlane(list[min(i + (wave * 64 + 256 * j) / (2 * D), kWindow - 1)].pos0) + kBlock - 1 > p_first) {
+        auto bad = [](uint32_t v) { return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u; };
+        if (__any(bad(vr[j][0]) || bad(vr[j][1]) || bad(vr[j][2]) || bad(vr[j][3])) && lane == 0) odd[i / kTilePages] = 1;
+      }
+    }
+  };
+
+  // ---- the queries at their positions, in units of the logits' powers of two
+  const float scale = rsqrtf(static_cast<float>(D)) * kLog2e;
+  bf16x8 q[D / 16];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    const bf16x8 x = __builtin_bit_cast(bf16x8, raw[i]), y = __builtin_bit_cast(bf16x8, raw[i + D / 32]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float cs, sn;
+      rot_cos_sin_fast(pos, inv_freq.f[16 * i + 8 * h + e], &cs, &sn);
+      const float u = to_float(x[e]), w = to_float(y[e]);
+      q[i][e] = static_cast<bf16_t>((u * cs - w * sn) * scale);
+      q[i + D / 32][e] = static_cast<bf16_t>((w * cs + u * sn) * scale);
+    }
+  }
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+  float m = -3.4028235e38f, l = 0.f;
+  // byte of this lane's key operand in an image: row of the block as token of its two pages; piece 2 kk + h is this one's, bits of kk flipped
+  const int k_row = (n >> 4) * kBlock + ((n >> 2) & 1) * 8 + ((n >> 3) & 1) * 4 + (n & 3);
+  const int k_byte = ((ks * kBlocks * 32 + k_row) * (D / 8) + (h ^ ((k_row & 3) | ((k_row >> 1) & 4)))) * 16, v_byte = (8 * D + ks * kBlocks * 4 * D + h * D + (n ^ (4 * h))) * 16;
+
+  // One tile.  ODD: one that was set aside.  p: the tile's pages, page lane % 4 in each lane.
+  auto compute = [&](auto set_aside, const u32x4* img, const Page& p) __attribute__((always_inline)) {
+    constexpr bool ODD = decltype(set_aside)::value;
+    const int b0 = ks * kBlocks;                                       // this wavefront's first 32-key block
+    f32x16 s[kBlocks];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
+    // (the operands' addresses are made here again: kept over the loop they would cost a register each)
+    const char* bytes = reinterpret_cast<const char*>(img);
+    int k_at = k_byte;
+    asm volatile("" : "+v"(k_at));
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        const bf16x8 k = *reinterpret_cast<const bf16x8*>(bytes + (k_at ^ (32 * kk)) + b * 64 * D);
+        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[kk], s[b], 0, 0, 0);
+      }
+    if (!__all(p.n_valid == kBlock && p.pos0 + kBlock - 1 <= p_min)) {
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const int pg = (b0 + b) * 2 + g;
+          const int seen = min(__shfl(p.n_valid, pg, 64) - 8 * h, pos - (__shfl(p.pos0, pg, 64) + 8 * h) + 1);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s[b][8 * g + e] = e < seen ? s[b][8 * g + e] : -INFINITY;
+        }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
+    if (__any(top > m + kSlack)) {
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float m_new = fmaxf(m, top), f = exp2f(m - m_new);
+      m = m_new;
+      l *= f;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) o[j] *= f;
+    }
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        bf16x8 w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = __builtin_amdgcn_exp2f(s[b][8 * g + e] - m);
+          l += x;
+          w[e] = static_cast<bf16_t>(x);
+        }
+        const int pg = (b0 + b) * 2 + g;
+        const char* v_at = bytes + v_byte + (2 * b + g) * 32 * D;
+        if constexpr (!ODD) {
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j)
+            o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(v_at + j * 512), w, o[j], 0, 0, 0);
+        } else {
+          // the values that are not finite leave the product and are added to the columns that see them
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) {
+            bf16x8 v = *reinterpret_cast<const bf16x8*>(v_at + j * 512);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = fabsf(to_float(v[e])) < INFINITY ? v[e] : static_cast<bf16_t>(0.f);
+            o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, o[j], 0, 0, 0);
+          }
+          const int first = __shfl(p.pos0, pg, 64);
+          const bf16_t* values = reinterpret_cast<const bf16_t*>(img + 8 * D + pg * 2 * D);
+#pragma unroll 1
+          for (int t = 0; t < kBlock; ++t) {
+            float weight = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) weight = t % 8 == e ? to_float(w[e]) : weight;
+            weight = __shfl(weight, n + 32 * (t >> 3), 64);
+            const bool sees = first + t <= pos;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const int d = 32 * j + 8 * (e >> 2) + 4 * h + (e & 3);
+                const float v = to_float(values[((t >> 3) * D + (d ^ (4 * (t >> 3)))) * 8 + (t & 7)]);
+                if (sees && !(fabsf(v) < INFINITY)) o[j][e] += weight * v;
+                asm volatile("" ::: "memory");                        // (one value in flight: this is rare, and registers are not)
+              }
+          }
+        }
+      }
+  };
+
+  // ---- the keys, until no column of the workgroup sees them
+  auto pages_at = [&](int i, int here) __attribute__((always_inline)) {
+    Page p = list[min(i + (lane & 3), kWindow - 1)];
+    if (i + (lane & 3) >= here) p.n_valid = 0;
+    return p;
+  };
+  for (int at = first_page; at < end_page; at += kWindow) {
+    if (at > first_page) list_pages(a, s_begin, s_end, at, list, scratch.segs, scratch.seg_end, scratch.wave_pages);
+    if (tid < kWindow / kTilePages) odd[tid] = 0;
+    const int in_range = min(end_page - at, kWindow);
+    // (pages are in the order of their positions; one that does not exist has no keys)
+    const int here = __syncthreads_count(tid < in_range && (list[tid].pos0 <= p_last || list[tid].n_valid == 0)), tiles = (here + kTilePages - 1) / kTilePages;
+    if (tiles > 0) {
+      load(0, here);
+      store(0, 0);
+      if (tiles > 1) load(kTilePages, here);
+    }
+    __syncthreads();
+    for (int t = 0; t < tiles; ++t) {
+      if (t + 1 < tiles) store((t + 1) & 1, (t + 1) * kTilePages);
+      if (t + 2 < tiles) load((t + 2) * kTilePages, here);
+      if (odd[t] == 0) compute(std::false_type(), image + (t & 1) * kImage, pages_at(t * kTilePages, here));
+      __syncthreads();
+    }
+    for (int t = 0; t < tiles; ++t)
+      if (odd[t] != 0) {
+        load(t * kTilePages, here);
+        store(0, t * kTilePages);
+        __syncthreads();
+        compute(std::true_type(), image, pages_at(t * kTilePages, here));
+        __syncthreads();
+      }
+  }
+
+  // ---- results
+  l += __shfl_xor(l, 32, 64);
+  float* mine = reinterpret_cast<float*>(image);
+  if constexpr (KS == 2) {
+    // the second stream's sums go through LDS to the first one's lanes: [value][lane]
+    __syncthreads();
+    if (ks == 1) {
+      float* to = mine + cw * (D / 2 + 2) * 64 + lane;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) to[(16 * j + e) * 64] = o[j][e];
+      to[(D / 2) * 64] = m;
+      to[(D / 2 + 1) * 64] = l;
+    }
+    __syncthreads();
+    if (ks == 1) return;
+    const float* from = mine + cw * (D / 2 + 2) * 64 + lane;
+    const float m1 = from[(D / 2) * 64], top = fmaxf(m, m1), f0 = exp2f(m - top), f1 = exp2f(m1 - top);
+    l = l * f0 + from[(D / 2 + 1) * 64] * f1;
+    m = top;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[j][e] = o[j][e] * f0 + from[(16 * j + e) * 64] * f1;
+  }
+  if (col >= n_cols) return;
+  const size_t at = static_cast<size_t>(row) * a.hq + kvh * group + my_col % group;
+#pragma unroll
+  for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      store_result<bf16_t, D>(a, at, split, n_splits, 32 * j + 8 * e + 4 * h, f32x4{o[j][4 * e], o[j][4 * e + 1], o[j][4 * e + 2], o[j][4 * e + 3]}, m, l);
+  if (split == 0 && kvh == 0 && my_col % group == 0 && h == 0) a.row_splits[row] = n_splits;
 }
 
 // Joins the ranges of one row and head: sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  The threads of a group of D / 4 take four dims
@@ -423,17 +727,21 @@ __global__ __launch_bounds__(256) void append_join_kernel(AppendArgs a) {
 
 // How the work of a call is divided: from host scalars alone.
 struct AppendPlan {
-  int nc, col_groups, n_splits, split_pages;
+  int cols;                           // columns of a workgroup: 16, 32 (append_split_kernel); 64, 128 (append_tile_kernel)
+  int col_groups, n_splits, split_pages;
+  long long groups;                   // workgroups
 };
 AppendPlan plan_append(const cc_ctx* ctx, int max_q_per_req, int n_requests, int max_ctx_tokens, int max_segs_per_req) {
   const long long cols = static_cast<long long>(max_q_per_req) * (ctx->cfg.n_q_heads / ctx->cfg.n_kv_heads);
   AppendPlan p;
-  p.nc = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
-  p.col_groups = static_cast<int>((cols + 16 * p.nc - 1) / (16 * p.nc));
-  const long long pages = max_ctx_tokens / kBlock + static_cast<long long>(max_segs_per_req), units = static_cast<long long>(p.col_groups) * ctx->cfg.n_kv_heads * n_requests;
-  const long long splits = std::max(1ll, std::min(2048 / std::max(1ll, units), (pages + 7) / 8));
-  p.split_pages = static_cast<int>((pages + splits - 1) / splits + 1) & ~1;
+  p.cols = cols <= 16 ? 16 : cols <= 32 || ctx->cfg.dtype != CC_BF16 ? 32 : cols <= 64 ? 64 : 128;
+  p.col_groups = static_cast<int>((cols + p.cols - 1) / p.cols);
+  const long long pages = max_ctx_tokens / kBlock + static_cast<long long>(max_segs_per_req), units = static_cast<long long>(ctx->cfg.n_kv_heads) * n_requests;
+  const long long target = p.cols <= 32 ? CC_T1 : CC_T2, least = p.cols <= 32 ? 8 : 16;
+  const long long splits = std::max(1ll, std::min(target / std::max(1ll, units * p.col_groups), (pages + least - 1) / least));
+  p.split_pages = static_cast<int>(((pages + splits - 1) / splits + 3) & ~3ll);
   p.n_splits = static_cast<int>((pages + p.split_pages - 1) / p.split_pages);
+  p.groups = (units * p.n_splits + 7) / 8 * 8 * p.col_groups;
   return p;
 }
 
@@ -506,10 +814,13 @@ size_t append_bytes(const cc_ctx* ctx, int n_q_tot, int max_q_per_req, int n_req
 
 template <typename T, int D>
 static void launch_append_t(const cc_ctx* ctx, const AppendArgs& a, const AppendPlan& p, int n_q_tot, hipStream_t stream) {
-  const dim3 grid(p.n_splits * p.col_groups, a.hkv, a.n_requests);
-  if (p.nc == 1) hipLaunchKernelGGL((append_split_kernel<T, D, 1>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
-  else if (p.nc == 2) hipLaunchKernelGGL((append_split_kernel<T, D, 2>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
-  else hipLaunchKernelGGL((append_split_kernel<T, D, 4>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
+  const dim3 grid(static_cast<unsigned>(p.groups));
+  if (p.cols == 16) hipLaunchKernelGGL((append_split_kernel<T, D, 1>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
+  if (p.cols == 32) hipLaunchKernelGGL((append_split_kernel<T, D, 2>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
+  if constexpr (sizeof(T) == 2) {
+    if (p.cols == 64) hipLaunchKernelGGL((append_tile_kernel<D, 2>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
+    if (p.cols == 128) hipLaunchKernelGGL((append_tile_kernel<D, 4>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
+  }
   if (p.n_splits > 1) hipLaunchKernelGGL((append_join_kernel<T, D>), dim3(n_q_tot, a.hq), dim3(256), 0, stream, a);
 }
 
@@ -535,7 +846,7 @@ void launch_append_attention(const cc_ctx* ctx, const void* q, const int32_t* sr
   float* part_o = static_cast<float*>(workspace);
   float* part_ml = part_o + static_cast<size_t>(n_q_tot) * hq * p.n_splits * d;
   const AppendArgs a{q, src_rows, q_pos, cu_q, k_pool, v_pool, block_tab, segs, req_seg_off, out, lse, vs, n_requests, n_blocks, hq, hkv,
-                     p.n_splits, p.split_pages, part_o, part_ml, reinterpret_cast<int32_t*>(part_ml + static_cast<size_t>(n_q_tot) * hq * p.n_splits * 2)};
+                     p.n_splits, p.split_pages, p.col_groups, part_o, part_ml, reinterpret_cast<int32_t*>(part_ml + static_cast<size_t>(n_q_tot) * hq * p.n_splits * 2)};
   if (bf && d == 128) launch_append_t<bf16_t, 128>(ctx, a, p, n_q_tot, stream);
   else if (bf) launch_append_t<bf16_t, 64>(ctx, a, p, n_q_tot, stream);
   else if (d == 128) launch_append_t<float, 128>(ctx, a, p, n_q_tot, stream);
