@@ -465,20 +465,27 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   const bf16_t *k_pool = static_cast<const bf16_t*>(a.k_pool) + head_off, *v_pool = static_cast<const bf16_t*>(a.v_pool) + head_off;
   const bf16_t* v_shared = static_cast<const bf16_t*>(a.vs.v_shared) + head_off;
   u32x4 kr[kStage], vr[kStage];
-  // the tile that begins at entry i of the list, `here` entries of which are this range's (a wavefront's pieces of one load lie in one page)
+  int listed = 0;                                                     // pages of the window that count
+  // A thread stages the same piece of every 256 / (2 D)-th page, so that page numbers are a wavefront's and addresses a sum with a constant.
+  constexpr int kApart = 128 / D;                                     // pages between a thread's
+  const int pg0 = wave * 64 / (2 * D), piece = tid % (2 * D), token = piece / (D / 8), half = piece & 1;
+  char* const put_k = reinterpret_cast<char*>(image) + ((pg0 * kBlock + token) * (D / 8) + (piece % (D / 8) ^ ((token & 3) | ((token >> 1) & 4)))) * 16;
+  char* const put_v = reinterpret_cast<char*>(image) + (8 * D + pg0 * 2 * D + half * D + ((piece >> 1) ^ (4 * half))) * 16;
+  // the tile that begins at entry i of the list, `here` entries of which are this range's
   auto load = [&](int i, int here) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < kStage; ++j) {
-      const int pg = (wave * 64 + 256 * j) / (2 * D), piece = (tid + 256 * j) % (2 * D);
-      const Page p = list[min(i + pg, kWindow - 1)];
+      const int at = i + pg0 + j * kApart;
+      const Page p = list[min(at, kWindow - 1)];
       const int blk = __builtin_amdgcn_readfirstlane(p.blk), value = __builtin_amdgcn_readfirstlane(p.value);
-      const int n_valid = i + pg >= here ? 0 : __builtin_amdgcn_readfirstlane(p.n_valid);
+      const int n_valid = at >= here ? 0 : __builtin_amdgcn_readfirstlane(p.n_valid);
       kr[j] = *reinterpret_cast<const u32x4*>(k_pool + blk * block_elems + piece * 8);
       const bf16_t* from = value >= 0 ? v_pool + value * block_elems : v_shared + (-1 - value) * block_elems;
       vr[j] = *reinterpret_cast<const u32x4*>(from + piece * 8);
       if (n_valid < kBlock) {                                         // padding slots: zeros, or 0 x what lies there would be a product
-        auto keep = [&](int e) { const int t = 8 * (piece & 1) + 2 * e; return (t < n_valid ? 0xffffu : 0u) | (t + 1 < n_valid ? 0xffff0000u : 0u); };
-        vr[j] &= u32x4{keep(0), keep(1), keep(2), keep(3)};
+        const int left = n_valid - 8 * half;                          // of this thread's eight tokens
+        auto keep = [&](int t) { return (t < left ? 0xffffu : 0u) | (t + 1 < left ? 0xffff0000u : 0u); };
+        vr[j] &= u32x4{keep(0), keep(2), keep(4), keep(6)};
       }
     }
   };
@@ -487,15 +494,16 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   auto store = [&](int buf, int i) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < kStage; ++j) {
-      const int at = tid + 256 * j, pg = at / (2 * D), piece = at % (2 * D);
-      const int t = pg * kBlock + piece / (D / 8), ch = piece % (D / 8);
-      image[buf * kImage + t * (D / 8) + (ch ^ ((t & 3) | ((t >> 1) & 4)))] = kr[j];
-      const int d = piece >> 1, half = piece & 1;
-      image[buf * kImage + 8 * D + pg * 2 * D + half * D + (d ^ (4 * half))] = vr[j];
-      if (__builtin_amdgcn_readfirstlane(list[min(i + (wave * 64 + 256 * j) / (2 * D), kWindow - 1)].pos0) + kBlock - 1 > p_first) {
-        auto bad = [](uint32_t v) { return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u; };
-        if (__any(bad(vr[j][0]) || bad(vr[j][1]) || bad(vr[j][2]) || bad(vr[j][3])) && lane == 0) odd[i / kTilePages] = 1;
-      }
+      *reinterpret_cast<u32x4*>(put_k + buf * (kImage * 16) + j * kApart * 32 * D) = kr[j];
+      *reinterpret_cast<u32x4*>(put_v + buf * (kImage * 16) + j * kApart * 32 * D) = vr[j];
+    }
+    // (a tile's last page is the one that lies furthest)
+    if (__builtin_amdgcn_readfirstlane(list[min(i + kTilePages - 1, kWindow - 1)].pos0) + kBlock - 1 > p_first || i + kTilePages > listed) {
+      auto bad = [](uint32_t v) { return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u; };
+      bool any = false;
+#pragma unroll
+      for (int j = 0; j < kStage; ++j) any |= bad(vr[j][0]) || bad(vr[j][1]) || bad(vr[j][2]) || bad(vr[j][3]);
+      if (__any(any) && lane == 0) odd[i / kTilePages] = 1;
     }
   };
 
@@ -598,6 +606,8 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
           const bf16_t* values = reinterpret_cast<const bf16_t*>(img + 8 * D + pg * 2 * D);
 #pragma unroll 1
           for (int t = 0; t < kBlock; ++t) {
+            int dim0 = 4 * h;
+            asm volatile("" : "+v"(dim0));
             float weight = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) weight = t % 8 == e ? to_float(w[e]) : weight;
@@ -607,7 +617,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
             for (int j = 0; j < D / 32; ++j)
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
-                const int d = 32 * j + 8 * (e >> 2) + 4 * h + (e & 3);
+                const int d = 32 * j + 8 * (e >> 2) + dim0 + (e & 3);
                 const float v = to_float(values[((t >> 3) * D + (d ^ (4 * (t >> 3)))) * 8 + (t & 7)]);
                 if (sees && !(fabsf(v) < INFINITY)) o[j][e] += weight * v;
                 asm volatile("" ::: "memory");                        // (one value in flight: this is rare, and registers are not)
@@ -629,6 +639,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     const int in_range = min(end_page - at, kWindow);
     // (pages are in the order of their positions; one that does not exist has no keys)
     const int here = __syncthreads_count(tid < in_range && (list[tid].pos0 <= p_last || list[tid].n_valid == 0)), tiles = (here + kTilePages - 1) / kTilePages;
+    listed = here;
     if (tiles > 0) {
       load(0, here);
       store(0, 0);
