@@ -692,6 +692,7 @@ int cc_append_attention(cc_ctx* ctx, const void* q, const void* k_new, const voi
   CC_REQUIRE(n_blocks > 0 && n_requests > 0 && n_segs > 0 && max_q_per_req > 0 && max_ctx_tokens > 0 && max_segs_per_req > 0,
              "sizes must be positive");
   CC_REQUIRE(n_requests <= 65535, "more than 65535 requests in one call");
+  CC_REQUIRE(static_cast<int64_t>(n_q_tot) * ctx->cfg.n_q_heads <= 0x7fffffff, "more than 2^31 - 1 rows and heads");
   CC_REQUIRE(n_blocks <= (1 << 27) - 1, "a pool of more than 2^27 - 1 blocks has slots beyond 32 bits");
   CC_REQUIRE(aligned16(q) && aligned16(k_new) && aligned16(v_new) && aligned16(k_pool) && aligned16(v_pool) && aligned16(out) && aligned16(segs),
              "tensors must be 16-byte aligned");
@@ -703,9 +704,9 @@ int cc_append_attention(cc_ctx* ctx, const void* q, const void* k_new, const voi
   cc::ValueSource vs;
   if (!value_source(ctx, fn, shared, &vs)) return CC_ERR_INVALID_ARG;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  cc::launch_rope_scatter(ctx, cc::ScatterJob{k_new, v_new, src_rows, q_pos, slot_map, n_q_tot, k_pool, v_pool, n_blocks, vs}, st);
   cc::launch_append_attention(ctx, q, src_rows, q_pos, cu_q, n_q_tot, max_q_per_req, k_pool, v_pool, n_blocks, block_tab, segs, req_seg_off,
-                              n_requests, max_ctx_tokens, max_segs_per_req, out, lse, workspace, st, vs);
+                              n_requests, max_ctx_tokens, max_segs_per_req, out, lse, workspace, st,
+                              cc::ScatterJob{k_new, v_new, src_rows, q_pos, slot_map, n_q_tot, k_pool, v_pool, n_blocks, vs});
   return cc::check_launch(ctx, fn);
 }
 

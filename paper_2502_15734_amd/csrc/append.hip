@@ -3,7 +3,7 @@
 // Bound by the bytes of the keys and values: a page of 16 tokens is read once for all rows and all heads of its group, and a row brings
 // 2 G multiply-adds per element read (G query heads on a KV head), far below what the matrix cores take.  So the rows and heads
 // of a group are the 16 columns of a matrix instruction (most of them empty when one token is written: they cost nothing), and the keys
-// are divided: a workgroup takes one (request, KV head, 16 NC columns, range of pages), its four wavefronts every fourth tile of
+// are divided: a workgroup takes one (request, KV head, 16 columns, range of pages), its four wavefronts every fourth tile of
 // the range, and merge at the end; a second kernel joins the ranges of a row.
 //
 // Layout: S^T = K Q^T and O^T = V^T P^T with lane = (n = lane % 16, g = lane / 16), column n.  No operand passes through LDS: the
@@ -22,12 +22,6 @@ namespace cc {
 
 namespace {
 
-#ifndef CC_T1
-#define CC_T1 512
-#endif
-#ifndef CC_T2
-#define CC_T2 512
-#endif
 constexpr float kSlack = 8.f;         // in powers of two
 constexpr int kWindow = 256;          // pages listed in LDS at a time
 constexpr float kLog2e = 1.4426950408889634f;
@@ -46,9 +40,13 @@ struct AppendArgs {
   // division of the work
   int n_splits, split_pages, col_groups;
   float *part_o, *part_ml;            // [row][head][split][D], [row][head][split][2]
+  // rows to write in front of the attention (k_new null: they are written already)
+  const void *k_new, *v_new;
+  const int32_t* slot_map;
   int32_t* row_splits;                // [row] ranges its request has (1: the output is written)
 };
 
+constexpr int kNowhere = -(1 << 30);  // position of an entry that is no page
 struct Page {
   int blk, pos0, n_valid, value;      // value: block of the own pool, or -1 - block of the shared one
 };
@@ -56,17 +54,18 @@ struct Page {
 __device__ __forceinline__ int pages_of(int tokens) { return (max(tokens, 0) + kBlock - 1) / kBlock; }
 
 // Pages [first, first + kWindow) of a request into list[] (thread i: page first + i), those behind its last one with n_valid 0;
-// returns the number of pages the request has.  Thread i also takes segment i of 256 at a time, whose page counts are scanned.
+// returns the number of pages the request has; *end_pos: the position behind its last token.  Thread i also takes segment i of 256 at a time, whose page counts are scanned.
 __device__ __forceinline__ int list_pages(const AppendArgs& a, int s_begin, int s_end, int first, Page* list, int4* segs, int* seg_end,
-                                          int* wave_pages) {
+                                          int* wave_pages, int* end_pos) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, want = first + tid;
-  Page page{0, 0, 0, 0};
+  Page page{0, kNowhere, 0, 0};
   int total = 0;
   for (int s0 = s_begin; s0 < s_end; s0 += 256) {
     const int s = s0 + tid;
     int4 mine{0, 0, 0, 0};
     if (s < s_end) mine = *reinterpret_cast<const int4*>(&a.segs[s].logical_start);     // start, tokens, table offset, (rows)
     const int n = pages_of(mine.y);
+    if (s == s_end - 1) *end_pos = mine.x + max(mine.y, 0);
     int end = n;
     for (int o = 1; o < 64; o <<= 1) {
       const int up = __shfl_up(end, o, 64);
@@ -106,6 +105,44 @@ __device__ __forceinline__ int list_pages(const AppendArgs& a, int s_begin, int 
   list[tid] = page;
   __syncthreads();
   return total;
+}
+
+// The request's new rows (up to kWriteRows) whose tokens lie in the `here` listed pages go into their slots: keys turned to their positions, values into
+// their column of the page.  The keys are divided by position, so one workgroup of each KV head writes a row, the one that goes on to read it (a
+// token's position may also fall behind the end of the segment in front, on the same page entry: then two write the same).  others: also
+// those whose position no segment holds.
+constexpr int kWriteRows = 16;
+template <typename T, int D>
+__device__ __forceinline__ void write_rows(const AppendArgs& a, const InvFreq& inv_freq, const Page* list, int here, bool others, int end_pos, int row0, int n_rows,
+                                           int kvh) {
+  __shared__ int owned[kWriteRows];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (tid < kWriteRows) owned[tid] = 0;
+  __syncthreads();
+  const int pos0 = tid < here ? list[tid].pos0 : kNowhere;
+  for (int i = 0; i < n_rows; ++i) {
+    const int p = a.q_pos[row0 + i];
+    if ((p >= pos0 && p - pos0 < kBlock) || (others && tid == 0 && (p < 0 || p >= end_pos))) owned[i] = 1;
+  }
+  __syncthreads();
+  for (int i = wave; i < n_rows; i += 4) {
+    if (owned[i] == 0) continue;
+    const int row = row0 + i, p = a.q_pos[row], slot = a.slot_map[row], src = a.src_rows != nullptr ? a.src_rows[row] : row;
+    if (slot < 0 || slot >= a.n_blocks * kBlock || lane >= D / 2) continue;
+    const size_t from = (static_cast<size_t>(src) * a.hkv + kvh) * D, head = (static_cast<size_t>(slot / kBlock) * a.hkv + kvh) * (kBlock * D);
+    const T *kn = static_cast<const T*>(a.k_new) + from, *vn = static_cast<const T*>(a.v_new) + from;
+    const float x = to_float(kn[lane]), y = to_float(kn[lane + D / 2]);
+    float c, s;
+    if (sizeof(T) == 2) rot_cos_sin_fast(p, inv_freq.f[lane], &c, &s);           // (the result is rounded to bf16)
+    else rot_cos_sin(p, inv_freq.f[lane], &c, &s);
+    T* ko = const_cast<T*>(static_cast<const T*>(a.k_pool)) + head + slot % kBlock * D;
+    T* vo = const_cast<T*>(static_cast<const T*>(a.v_pool)) + head + slot % kBlock;
+    ko[lane] = from_float<T>(x * c - y * s);
+    ko[lane + D / 2] = from_float<T>(y * c + x * s);
+    vo[lane * kBlock] = vn[lane];
+    vo[(lane + D / 2) * kBlock] = vn[lane + D / 2];
+  }
+  __syncthreads();                                     // (the workgroup's loads behind it see the rows)
 }
 
 template <typename T, int D> struct Tile;           // operands of one tile of keys
@@ -214,8 +251,8 @@ __device__ __forceinline__ void store_result(const AppendArgs& a, size_t at, int
   }
 }
 
-// One (range of pages, KV head and 16 NC columns, request).  Column c is head c % G of the request's row c / G.
-template <typename T, int D, int NC>
+// One (range of pages, KV head and 16 columns, request).  Column c is head c % G of the request's row c / G.
+template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvFreq inv_freq) {
   typedef Tile<T, D> Keys;
   typedef typename Keys::Piece Piece;
@@ -225,70 +262,60 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
   const Unit unit = unit_of(a);
   const int r = unit.req, kvh = unit.kvh, split = unit.split, group = a.hq / a.hkv;
   if (r >= a.n_requests) return;
-  const int col0 = unit.col_group * 16 * NC, row0 = a.cu_q[r], n_cols = (a.cu_q[r + 1] - row0) * group;
+  const int col0 = unit.col_group * 16, row0 = a.cu_q[r], n_cols = (a.cu_q[r + 1] - row0) * group;
   if (col0 >= n_cols) return;
   const int s_begin = a.req_seg_off[r], s_end = a.req_seg_off[r + 1];
 
   union Shared {
-    struct { Page list[kWindow]; int4 segs[256]; int seg_end[256]; int wave_pages[4]; } in;
+    struct { Page list[kWindow]; int4 segs[256]; int seg_end[256]; int wave_pages[4]; int end_pos; } in;
     struct { float o[4][16][kRow]; float m[4][16], l[4][16]; } out;
   };
   __shared__ Shared sh;
 
   // ---- positions of the columns, and the rows themselves (loads first, turned later)
-  int pos[NC], p_min = 0x7fffffff, p_max = -1;
-  Piece q[NC][kQ];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int col = col0 + 16 * c + n, row = row0 + min(col, n_cols - 1) / group;
-    pos[c] = a.q_pos[row];
-    if (col < n_cols) { p_min = min(p_min, pos[c]); p_max = max(p_max, pos[c]); }
+  // (columns behind the last repeat its row)
+  Piece q[kQ];
+  const int my_col = min(col0 + n, n_cols - 1), pos = a.q_pos[row0 + my_col / group];
+  {
+    const int row = row0 + my_col / group;
     const int src = a.src_rows != nullptr ? a.src_rows[row] : row;
-    const T* qp = static_cast<const T*>(a.q) + (static_cast<size_t>(src) * a.hq + kvh * group + min(col, n_cols - 1) % group) * D + kPer * g;
+    const T* qp = static_cast<const T*>(a.q) + (static_cast<size_t>(src) * a.hq + kvh * group + my_col % group) * D + kPer * g;
 #pragma unroll
-    for (int i = 0; i < kQ; ++i) q[c][i] = *reinterpret_cast<const Piece*>(qp + 4 * kPer * i);
+    for (int i = 0; i < kQ; ++i) q[i] = *reinterpret_cast<const Piece*>(qp + 4 * kPer * i);
   }
-  p_min = wave_min_i(p_min);
-  p_max = wave_max_i(p_max);
-
   const size_t block_elems = static_cast<size_t>(a.hkv) * kBlock * D, head_off = static_cast<size_t>(kvh) * kBlock * D;
   const T *k_pool = static_cast<const T*>(a.k_pool), *v_pool = static_cast<const T*>(a.v_pool), *v_shared = static_cast<const T*>(a.vs.v_shared);
-  float m[NC], l[NC];
-  f32x4 o[NC][D / 16];
+  float m = -3.4028235e38f, l = 0.f;
+  f32x4 o[D / 16];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    m[c] = -3.4028235e38f;
-    l[c] = 0.f;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) o[c][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int i = 0; i < D / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   const int first_page = split * a.split_pages;
-  int n_pages = list_pages(a, s_begin, s_end, first_page, sh.in.list, sh.in.segs, sh.in.seg_end, sh.in.wave_pages);
+  int n_pages = list_pages(a, s_begin, s_end, first_page, sh.in.list, sh.in.segs, sh.in.seg_end, sh.in.wave_pages, &sh.in.end_pos);
   if (first_page >= max(n_pages, 1)) return;                                        // (the same in all wavefronts)
   const int n_splits = min((max(n_pages, 1) + a.split_pages - 1) / a.split_pages, a.n_splits);
   const int end_page = split == a.n_splits - 1 ? n_pages : min(n_pages, first_page + a.split_pages);
 
+  const int p_min = wave_min_i(pos), p_max = wave_max_i(pos);             // (waited for behind the list's loads)
+
   // ---- the queries at their positions, in units of the logits' powers of two
   const float scale = rsqrtf(static_cast<float>(D)) * kLog2e;
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
+  for (int i = 0; i < kQ / 2; ++i) {
+    float x[kPer], y[kPer];
 #pragma unroll
-    for (int i = 0; i < kQ / 2; ++i) {
-      float x[kPer], y[kPer];
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        float cs, sn;
-        const double freq = inv_freq.f[4 * kPer * i + kPer * g + e];
-        if (sizeof(T) == 2) rot_cos_sin_fast(pos[c], freq, &cs, &sn);          // (the result is rounded to bf16)
-        else rot_cos_sin(pos[c], freq, &cs, &sn);
-        const float u = to_float(q[c][i][e]), w = to_float(q[c][i + kQ / 2][e]);
-        x[e] = (u * cs - w * sn) * scale;
-        y[e] = (w * cs + u * sn) * scale;
-      }
-      q[c][i] = Keys::piece(x);
-      q[c][i + kQ / 2] = Keys::piece(y);
+    for (int e = 0; e < kPer; ++e) {
+      float cs, sn;
+      const double freq = inv_freq.f[4 * kPer * i + kPer * g + e];
+      if (sizeof(T) == 2) rot_cos_sin_fast(pos, freq, &cs, &sn);          // (the result is rounded to bf16)
+      else rot_cos_sin(pos, freq, &cs, &sn);
+      const float u = to_float(q[i][e]), w = to_float(q[i + kQ / 2][e]);
+      x[e] = (u * cs - w * sn) * scale;
+      y[e] = (w * cs + u * sn) * scale;
     }
+    q[i] = Keys::piece(x);
+    q[i + kQ / 2] = Keys::piece(y);
+  }
 
   auto take = [&](Keys& t, const Page& held) __attribute__((always_inline)) {
     const int tok0 = Keys::token_of(lane), first = held.pos0 + tok0;       // of this lane's tokens
@@ -307,53 +334,50 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
         }
       apart = __any(odd);
     }
+    float s[kTok];
+    t.logits(q, s);
+    if (!whole) {
+      const int seen = min(held.n_valid - tok0, pos - first + 1);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      float s[kTok];
-      t.logits(q[c], s);
-      if (!whole) {
-        const int seen = min(held.n_valid - tok0, pos[c] - first + 1);
+      for (int e = 0; e < kTok; ++e) s[e] = e < seen ? s[e] : -INFINITY;
+    }
+    float top = s[0];
 #pragma unroll
-        for (int e = 0; e < kTok; ++e) s[e] = e < seen ? s[e] : -INFINITY;
-      }
-      float top = s[0];
+    for (int e = 1; e < kTok; ++e) top = fmaxf(top, s[e]);
+    if (__any(top > m + kSlack)) {
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float m_new = fmaxf(m, top), f = exp2f(m - m_new);
+      m = m_new;
+      l *= f;
 #pragma unroll
-      for (int e = 1; e < kTok; ++e) top = fmaxf(top, s[e]);
-      if (__any(top > m[c] + kSlack)) {
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float m_new = fmaxf(m[c], top), f = exp2f(m[c] - m_new);
-        m[c] = m_new;
-        l[c] *= f;
+      for (int i = 0; i < D / 16; ++i) o[i] *= f;
+    }
+    float p[kTok], sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) o[c][i] *= f;
-      }
-      float p[kTok], sum = 0.f;
+    for (int e = 0; e < kTok; ++e) { p[e] = __builtin_amdgcn_exp2f(s[e] - m); sum += p[e]; }
+    l += sum;
+    if (!apart) {
+      const Piece w = Keys::piece(p);
 #pragma unroll
-      for (int e = 0; e < kTok; ++e) { p[e] = __builtin_amdgcn_exp2f(s[e] - m[c]); sum += p[e]; }
-      l[c] += sum;
-      if (!apart) {
-        const Piece w = Keys::piece(p);
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) o[c][i] = Keys::add_values(t.v[i], w, o[c][i]);
-      } else {
-        // 0 x value would reach the columns that do not see it: one column at a time
+      for (int i = 0; i < D / 16; ++i) o[i] = Keys::add_values(t.v[i], w, o[i]);
+    } else {
+      // 0 x value would reach the columns that do not see it: one column at a time
 #pragma unroll 1
-        for (int k = 0; k < 16; ++k) {
-          const int seen = __shfl(pos[c], k, 16) - first + 1;
-          float only[kTok];
+      for (int k = 0; k < 16; ++k) {
+        const int seen = __shfl(pos, k, 16) - first + 1;
+        float only[kTok];
 #pragma unroll
-          for (int e = 0; e < kTok; ++e) only[e] = n == k ? p[e] : 0.f;
-          const Piece w = Keys::piece(only);
+        for (int e = 0; e < kTok; ++e) only[e] = n == k ? p[e] : 0.f;
+        const Piece w = Keys::piece(only);
 #pragma unroll
-          for (int i = 0; i < D / 16; ++i) {
-            Piece v = t.v[i];
+        for (int i = 0; i < D / 16; ++i) {
+          Piece v = t.v[i];
 #pragma unroll
-            for (int e = 0; e < kTok; ++e)
-              if (e >= seen) v[e] = static_cast<T>(0.f);
-            const f32x4 add = Keys::add_values(v, w, f32x4{0.f, 0.f, 0.f, 0.f});
-            if (n == k) o[c][i] += add;
-          }
+          for (int e = 0; e < kTok; ++e)
+            if (e >= seen) v[e] = static_cast<T>(0.f);
+          const f32x4 add = Keys::add_values(v, w, f32x4{0.f, 0.f, 0.f, 0.f});
+          if (n == k) o[i] += add;
         }
       }
     }
@@ -362,6 +386,7 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
   // ---- the keys: every fourth tile of the window is this wavefront's
   for (int at = first_page;;) {
     const int here = min(end_page - at, kWindow);
+    if (a.k_new != nullptr) write_rows<T, D>(a, inv_freq, sh.in.list, here, split == 0 && at == first_page, s_end > s_begin ? sh.in.end_pos : 0, row0, n_cols / group, kvh);
     for (int i = wave * Keys::kPages; i < here; i += 4 * Keys::kPages) {
       Keys t;
       t.load(k_pool, v_pool, v_shared, sh.in.list + i, block_elems, head_off, lane);
@@ -372,38 +397,35 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
     at += kWindow;
     __syncthreads();
     if (at >= end_page) break;
-    list_pages(a, s_begin, s_end, at, sh.in.list, sh.in.segs, sh.in.seg_end, sh.in.wave_pages);
+    list_pages(a, s_begin, s_end, at, sh.in.list, sh.in.segs, sh.in.seg_end, sh.in.wave_pages, &sh.in.end_pos);
   }
 
   // ---- the four wavefronts' sums, and the result of this range
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (g == 0) { sh.out.m[wave][n] = m; sh.out.l[wave][n] = l; }
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    l[c] += __shfl_xor(l[c], 16, 64);
-    l[c] += __shfl_xor(l[c], 32, 64);
-    if (g == 0) { sh.out.m[wave][n] = m[c]; sh.out.l[wave][n] = l[c]; }
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&sh.out.o[wave][n][16 * i + 4 * g]) = o[c][i];
-    __syncthreads();
-    for (int i = tid; i < 16 * (D / 4); i += 256) {
-      const int k = i / (D / 4), d = i % (D / 4) * 4, col = col0 + 16 * c + k;
-      if (col < n_cols) {
-        float top = sh.out.m[0][k];
-        for (int w = 1; w < 4; ++w) top = fmaxf(top, sh.out.m[w][k]);
-        float sum = 0.f;
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        for (int w = 0; w < 4; ++w) {
-          const float f = exp2f(sh.out.m[w][k] - top);
-          sum += f * sh.out.l[w][k];
-          v += *reinterpret_cast<const f32x4*>(&sh.out.o[w][k][d]) * f;
-        }
-        const int row = row0 + col / group;
-        const size_t at = static_cast<size_t>(row) * a.hq + kvh * group + col % group;
-        store_result<T, D>(a, at, split, n_splits, d, v, top, sum);
-        if (split == 0 && d == 0 && kvh == 0 && col % group == 0) a.row_splits[row] = n_splits;
+  for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&sh.out.o[wave][n][16 * i + 4 * g]) = o[i];
+  __syncthreads();
+  for (int i = tid; i < 16 * (D / 4); i += 256) {
+    const int k = i / (D / 4), d = i % (D / 4) * 4, col = col0 + k;
+    if (col < n_cols) {
+      float top = sh.out.m[0][k];
+      for (int w = 1; w < 4; ++w) top = fmaxf(top, sh.out.m[w][k]);
+      float sum = 0.f;
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      for (int w = 0; w < 4; ++w) {
+        const float f = exp2f(sh.out.m[w][k] - top);
+        sum += f * sh.out.l[w][k];
+        v += *reinterpret_cast<const f32x4*>(&sh.out.o[w][k][d]) * f;
       }
+      const int row = row0 + col / group;
+      const size_t at = static_cast<size_t>(row) * a.hq + kvh * group + col % group;
+      store_result<T, D>(a, at, split, n_splits, d, v, top, sum);
+      if (split == 0 && d == 0 && kvh == 0 && col % group == 0) a.row_splits[row] = n_splits;
     }
-    __syncthreads();
   }
+  __syncthreads();
 }
 
 // ---- many columns -------------------------------------------------------------------------------
@@ -439,6 +461,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   __shared__ int odd[kWindow / kTilePages];
   __shared__ int2 edge_pos[4];
   struct Scratch { int4 segs[256]; int seg_end[256]; int wave_pages[4]; };
+  __shared__ int end_pos;
   Scratch& scratch = *reinterpret_cast<Scratch*>(image);               // (while a list is made no image is in use)
 
   const int col = wg_col + 32 * cw + n, my_col = min(col, n_cols - 1), row = row0 + my_col / group, pos = a.q_pos[row];
@@ -450,7 +473,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     for (int i = 0; i < D / 16; ++i) raw[i] = *reinterpret_cast<const u32x4*>(qp + 16 * i);
   }
   const int first_page = split * a.split_pages;
-  const int n_pages = list_pages(a, s_begin, s_end, first_page, list, scratch.segs, scratch.seg_end, scratch.wave_pages);
+  const int n_pages = list_pages(a, s_begin, s_end, first_page, list, scratch.segs, scratch.seg_end, scratch.wave_pages, &end_pos);
   if (first_page >= max(n_pages, 1)) return;
   const int n_splits = min((max(n_pages, 1) + a.split_pages - 1) / a.split_pages, a.n_splits);
   const int end_page = split == a.n_splits - 1 ? n_pages : min(n_pages, first_page + a.split_pages);
@@ -633,10 +656,11 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     if (i + (lane & 3) >= here) p.n_valid = 0;
     return p;
   };
-  for (int at = first_page; at < end_page; at += kWindow) {
-    if (at > first_page) list_pages(a, s_begin, s_end, at, list, scratch.segs, scratch.seg_end, scratch.wave_pages);
+  for (int at = first_page; at == first_page || at < end_page; at += kWindow) {
+    if (at > first_page) list_pages(a, s_begin, s_end, at, list, scratch.segs, scratch.seg_end, scratch.wave_pages, &end_pos);
     if (tid < kWindow / kTilePages) odd[tid] = 0;
     const int in_range = min(end_page - at, kWindow);
+    if (a.k_new != nullptr) write_rows<bf16_t, D>(a, inv_freq, list, in_range, split == 0 && at == first_page, s_end > s_begin ? end_pos : 0, row0, n_cols / group, kvh);
     // (pages are in the order of their positions; one that does not exist has no keys)
     const int here = __syncthreads_count(tid < in_range && (list[tid].pos0 <= p_last || list[tid].n_valid == 0)), tiles = (here + kTilePages - 1) / kTilePages;
     listed = here;
@@ -698,57 +722,84 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   if (split == 0 && kvh == 0 && my_col % group == 0 && h == 0) a.row_splits[row] = n_splits;
 }
 
-// Joins the ranges of one row and head: sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  The threads of a group of D / 4 take four dims
-// each, the groups every so-manieth range.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void append_join_kernel(AppendArgs a) {
+// Joins the ranges of a row and head: sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  D / 4 threads take four dims each; where there are many
+// ranges (WIDE) the groups of such threads of a workgroup share one row and head, every so-manieth range each, otherwise they take one each.
+template <typename T, int D, bool WIDE>
+__global__ __launch_bounds__(256) void append_join_kernel(AppendArgs a, int n_items) {
   constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
-  __shared__ float top_of[4], sum_of[kGroups];
-  __shared__ f32x4 part[kGroups][kLanes];
-  const int row = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, lane = tid % kLanes, grp = tid / kLanes;
+  __shared__ f32x4 part[WIDE ? kGroups : 1][kLanes];
+  __shared__ float2 sum_of[WIDE ? kGroups : 1];
+  const int tid = threadIdx.x, lane = tid % kLanes, grp = tid / kLanes;
+  const int at = WIDE ? blockIdx.x : blockIdx.x * kGroups + grp;             // row and head
+  if (at >= n_items) return;
+  const int row = at / a.hq;
   if (row >= a.cu_q[a.n_requests]) return;
-  const int ns = a.row_splits[row];
+  const int ns = a.row_splits[row], step = WIDE ? kGroups : 1;
   if (ns <= 1) return;
-  const size_t at = static_cast<size_t>(row) * a.hq + h;
-  const float* ml = a.part_ml + at * a.n_splits * 2;
-  float top = -INFINITY;
-  for (int s = tid; s < ns; s += 256) top = fmaxf(top, ml[2 * s]);
-  top = wave_max(top);
-  if ((tid & 63) == 0) top_of[tid >> 6] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
-  float sum = 0.f;
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + static_cast<size_t>(at) * a.n_splits;
+  const float* po = a.part_o + static_cast<size_t>(at) * a.n_splits * D + 4 * lane;
+  float top = -INFINITY, sum = 0.f;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int s = grp; s < ns; s += kGroups) {
-    const float f = exp2f(ml[2 * s] - top);
-    sum += f * ml[2 * s + 1];
-    v += *reinterpret_cast<const f32x4*>(a.part_o + (at * a.n_splits + s) * D + 4 * lane) * f;
-  }
-  part[grp][lane] = v;
-  if (lane == 0) sum_of[grp] = sum;
-  __syncthreads();
-  if (grp != 0) return;
-  for (int k = 1; k < kGroups; ++k) { v += part[k][lane]; sum += sum_of[k]; }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  T* op = static_cast<T*>(a.out) + at * D + 4 * lane;
+  constexpr int kAhead = 4;                                                 // ranges whose loads are under way together
+  for (int s0 = WIDE ? grp : 0; s0 < ns; s0 += kAhead * step) {
+    float2 x[kAhead];
+    f32x4 y[kAhead];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) op[e] = from_float<T>(v[e] * inv);
-  if (lane == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : top / kLog2e + logf(sum);
+    for (int i = 0; i < kAhead; ++i) {
+      const int s = min(s0 + i * step, ns - 1);
+      x[i] = ml[s];
+      y[i] = *reinterpret_cast<const f32x4*>(po + static_cast<size_t>(s) * D);
+    }
+    float t = top;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (s0 + i * step < ns) t = fmaxf(t, x[i].x);
+    const float f = exp2f(top - t);
+    top = t;
+    sum *= f;
+    v *= f;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const float w = s0 + i * step < ns ? exp2f(x[i].x - t) : 0.f;
+      sum += w * x[i].y;
+      v += y[i] * w;
+    }
+  }
+  if constexpr (WIDE) {
+    part[grp][lane] = v;
+    if (lane == 0) sum_of[grp] = make_float2(top, sum);
+    __syncthreads();
+    if (grp != 0) return;
+    float t = top;
+#pragma unroll
+    for (int k = 1; k < kGroups; ++k) t = fmaxf(t, sum_of[k].x);
+    const float f = exp2f(top - t);
+    sum *= f;
+    v *= f;
+#pragma unroll
+    for (int k = 1; k < kGroups; ++k) {
+      const float w = exp2f(sum_of[k].x - t);
+      sum += w * sum_of[k].y;
+      v += part[k][lane] * w;
+    }
+    top = t;
+  }
+  store_result<T, D>(a, at, 0, 1, 4 * lane, v, top, sum);
 }
 
 // How the work of a call is divided: from host scalars alone.
 struct AppendPlan {
-  int cols;                           // columns of a workgroup: 16, 32 (append_split_kernel); 64, 128 (append_tile_kernel)
+  int cols;                           // columns of a workgroup: 16 (append_split_kernel); 64, 128 (append_tile_kernel)
   int col_groups, n_splits, split_pages;
   long long groups;                   // workgroups
 };
 AppendPlan plan_append(const cc_ctx* ctx, int max_q_per_req, int n_requests, int max_ctx_tokens, int max_segs_per_req) {
   const long long cols = static_cast<long long>(max_q_per_req) * (ctx->cfg.n_q_heads / ctx->cfg.n_kv_heads);
   AppendPlan p;
-  p.cols = cols <= 16 ? 16 : cols <= 32 || ctx->cfg.dtype != CC_BF16 ? 32 : cols <= 64 ? 64 : 128;
+  p.cols = cols <= 16 || ctx->cfg.dtype != CC_BF16 ? 16 : cols <= 64 ? 64 : 128;
   p.col_groups = static_cast<int>((cols + p.cols - 1) / p.cols);
   const long long pages = max_ctx_tokens / kBlock + static_cast<long long>(max_segs_per_req), units = static_cast<long long>(ctx->cfg.n_kv_heads) * n_requests;
-  const long long target = p.cols <= 32 ? CC_T1 : CC_T2, least = p.cols <= 32 ? 8 : 16;
+  const long long target = 512, least = p.cols == 16 ? 8 : 16;
   const long long splits = std::max(1ll, std::min(target / std::max(1ll, units * p.col_groups), (pages + least - 1) / least));
   p.split_pages = static_cast<int>(((pages + splits - 1) / splits + 3) & ~3ll);
   p.n_splits = static_cast<int>((pages + p.split_pages - 1) / p.split_pages);
@@ -826,22 +877,25 @@ size_t append_bytes(const cc_ctx* ctx, int n_q_tot, int max_q_per_req, int n_req
 template <typename T, int D>
 static void launch_append_t(const cc_ctx* ctx, const AppendArgs& a, const AppendPlan& p, int n_q_tot, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(p.groups));
-  if (p.cols == 16) hipLaunchKernelGGL((append_split_kernel<T, D, 1>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
-  if (p.cols == 32) hipLaunchKernelGGL((append_split_kernel<T, D, 2>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
+  if (p.cols == 16) hipLaunchKernelGGL((append_split_kernel<T, D>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
   if constexpr (sizeof(T) == 2) {
     if (p.cols == 64) hipLaunchKernelGGL((append_tile_kernel<D, 2>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
     if (p.cols == 128) hipLaunchKernelGGL((append_tile_kernel<D, 4>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
   }
-  if (p.n_splits > 1) hipLaunchKernelGGL((append_join_kernel<T, D>), dim3(n_q_tot, a.hq), dim3(256), 0, stream, a);
+  const int n_items = n_q_tot * a.hq;
+  if (p.n_splits > 8) hipLaunchKernelGGL((append_join_kernel<T, D, true>), dim3(n_items), dim3(256), 0, stream, a, n_items);
+  else if (p.n_splits > 1) hipLaunchKernelGGL((append_join_kernel<T, D, false>), dim3((n_items + 1024 / D - 1) / (1024 / D)), dim3(256), 0, stream, a, n_items);
 }
 
 void launch_append_attention(const cc_ctx* ctx, const void* q, const int32_t* src_rows, const int32_t* q_pos, const int32_t* cu_q, int n_q_tot,
                              int max_q_per_req, const void* k_pool, const void* v_pool, int n_blocks, const int32_t* block_tab,
                              const cc_segment* segs, const int32_t* req_seg_off, int n_requests, int max_ctx_tokens, int max_segs_per_req,
-                             void* out, float* lse, void* workspace, hipStream_t stream, const ValueSource& vs) {
+                             void* out, float* lse, void* workspace, hipStream_t stream, const ScatterJob& scatter) {
+  const ValueSource& vs = scatter.vs;
   const bool bf = ctx->cfg.dtype == CC_BF16;
   const int d = ctx->cfg.head_dim, hq = ctx->cfg.n_q_heads, hkv = ctx->cfg.n_kv_heads;
   if (ctx->impl == CC_IMPL_SCALAR) {
+    launch_rope_scatter(ctx, scatter, stream);
 #define CC_LAUNCH(T, D)                                                                                                          \
   hipLaunchKernelGGL((append_scalar_kernel<T, D>), dim3(n_q_tot, hq), dim3(64), 0, stream, static_cast<const T*>(q), src_rows, q_pos, \
                      cu_q, n_requests, static_cast<const T*>(k_pool), static_cast<const T*>(v_pool), n_blocks, block_tab, segs,      \
@@ -854,10 +908,15 @@ void launch_append_attention(const cc_ctx* ctx, const void* q, const int32_t* sr
     return;
   }
   const AppendPlan p = plan_append(ctx, max_q_per_req, n_requests, max_ctx_tokens, max_segs_per_req);
+  // Few rows are written by the workgroups that read them, which saves a launch (5 to 9 us); not into pages whose values may still be in
+  // the chunk store: those are copied whole, for all KV heads at once.
+  const bool write = p.col_groups == 1 && max_q_per_req <= kWriteRows && vs.v_map == nullptr;
+  if (!write) launch_rope_scatter(ctx, scatter, stream);
   float* part_o = static_cast<float*>(workspace);
   float* part_ml = part_o + static_cast<size_t>(n_q_tot) * hq * p.n_splits * d;
   const AppendArgs a{q, src_rows, q_pos, cu_q, k_pool, v_pool, block_tab, segs, req_seg_off, out, lse, vs, n_requests, n_blocks, hq, hkv,
-                     p.n_splits, p.split_pages, p.col_groups, part_o, part_ml, reinterpret_cast<int32_t*>(part_ml + static_cast<size_t>(n_q_tot) * hq * p.n_splits * 2)};
+                     p.n_splits, p.split_pages, p.col_groups, part_o, part_ml, write ? scatter.k_new : nullptr, scatter.v_new, scatter.slot_map,
+                     reinterpret_cast<int32_t*>(part_ml + static_cast<size_t>(n_q_tot) * hq * p.n_splits * 2)};
   if (bf && d == 128) launch_append_t<bf16_t, 128>(ctx, a, p, n_q_tot, stream);
   else if (bf) launch_append_t<bf16_t, 64>(ctx, a, p, n_q_tot, stream);
   else if (d == 128) launch_append_t<float, 128>(ctx, a, p, n_q_tot, stream);

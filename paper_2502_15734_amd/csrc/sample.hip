@@ -111,20 +111,19 @@ struct Cut {              // the ranks above it: logits above key, and the first
   unsigned ties;
 };
 
-constexpr int kWaves = 16, kThreads = 64 * kWaves;   // of the kernel with a workgroup per row
-
+template <int W>
 struct RowShared {
   unsigned count[256];
   unsigned long long mass[256];
-  unsigned wave_ties[kWaves], wave_kept[kWaves];
-  unsigned long long wave_mass[kWaves];
+  unsigned wave_ties[W], wave_kept[W];
+  unsigned long long wave_mass[W];
   unsigned found_digit, found_count;
   unsigned long long found_mass;
 };
 
 // The whole row by one workgroup, whatever its logits.  top: its largest one.
-template <typename T>
-__device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const RowSettings& s, uint32_t top, RowShared& sh) {
+template <typename T, int W>
+__device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const RowSettings& s, uint32_t top, RowShared<W>& sh) {
   unsigned *count = sh.count, *wave_ties = sh.wave_ties, *wave_kept = sh.wave_kept;
   unsigned long long *mass = sh.mass, *wave_mass = sh.wave_mass;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = a.vocab;
@@ -138,7 +137,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const R
     for (int digit = 3; digit >= 0; --digit) {
       if (tid < 256) { count[tid] = 0; mass[tid] = 0; }
       __syncthreads();
-      for (int i = tid; i < n; i += 64 * kWaves) {
+      for (int i = tid; i < n; i += 64 * W) {
         const uint32_t k = key_at<T>(a, row, i);
         if (k <= kKeyNone || (digit < 3 && (k >> (8 * digit + 8)) != prefix)) continue;
         atomicAdd(&count[(k >> (8 * digit)) & 255], 1u);
@@ -185,7 +184,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const R
   }
 
   // ---- the draw, in the order of the indexes: a wavefront owns a contiguous share
-  const int share = (n + kWaves - 1) / kWaves, i0 = wave * share, i1 = min(n, i0 + share);
+  const int share = (n + W - 1) / W, i0 = wave * share, i1 = min(n, i0 + share);
   auto weight = [&](uint32_t k) {
     const double w = k > kKeyNone ? weight_of(k, top, s.inv_t) : 0.0;
     return w >= s.min_p || k == top ? w : 0.0;
@@ -208,7 +207,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const R
   __syncthreads();
   unsigned ties_before = 0, n_kept = 0, first_ties = 0;
   unsigned long long total = 0;
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < W; ++w) {
     const unsigned left = cut.ties > ties_before ? cut.ties - ties_before : 0, t = tie_in ? min(left, wave_ties[w]) : 0;
     if (w == wave) first_ties = ties_before;
     n_kept += wave_kept[w] + t;
@@ -219,7 +218,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const R
   unsigned long long before = 0;
   unsigned tb = 0;
   int mine = -1;
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < W; ++w) {
     const unsigned left = cut.ties > tb ? cut.ties - tb : 0, t = tie_in ? min(left, wave_ties[w]) : 0;
     const unsigned long long m = wave_mass[w] + each * t;
     tb += wave_ties[w];
@@ -286,17 +285,31 @@ struct RowReader {
     shift = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
     vocab = a.vocab;
   }
-  // keys of the elements e .. e + kPer (e a multiple of kPer); what is not of the row gives kKeyNone and is not read
-  __device__ __forceinline__ void keys(int e, uint32_t (&k)[kPer]) const {
-    const int i = e - shift;
-    if (i >= 0 && i + kPer <= vocab) {
-      T v[kPer];
-      *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(row + i);
+  typedef __attribute__((__vector_size__(16))) T Piece;
+  // f(key, index) for the row's elements in [e0 + lane kPer, e1) in steps of `step` elements (multiples of kPer), in the order of the indexes; kAhead
+  // pieces are loaded before the first is used.  Only the row's own logits are read, -inf and NaN passed over.
+  template <typename F>
+  __device__ __forceinline__ void each(int e0, int e1, int step, F&& f) const {
+    constexpr int kAhead = 4;
+    for (int e = e0; e < e1; e += kAhead * step) {
+      Piece v[kAhead];
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) k[j] = logit_key(to_float(v[j]));
-    } else {
+      for (int a = 0; a < kAhead; ++a) {
+        const int i = e + a * step - shift;
+        if (i >= 0 && i + kPer <= vocab && e + a * step < e1) v[a] = *reinterpret_cast<const Piece*>(row + i);
+      }
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) k[j] = i + j >= 0 && i + j < vocab ? logit_key(to_float(row[i + j])) : kKeyNone;
+      for (int a = 0; a < kAhead; ++a) {
+        const int i = e + a * step - shift;
+        if (e + a * step >= e1) break;
+        const bool whole = i >= 0 && i + kPer <= vocab;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+          if (!whole && (i + j < 0 || i + j >= vocab)) continue;
+          const uint32_t k = logit_key(to_float(whole ? v[a][j] : row[i + j]));
+          if (k > kKeyNone) f(k, i + j);
+        }
+      }
     }
   }
 };
@@ -427,16 +440,10 @@ __global__ __launch_bounds__(256) void sample_max_kernel(SampleArgs a, SamplePla
   uint32_t top = 0, low = 0xffffffffu;
   int at = 0x7fffffff;
   const int e1 = min((part + 1) * plan.part_len, a.vocab + in.shift);
-#pragma unroll 4
-  for (int e = part * plan.part_len + tid * kPer; e < e1; e += 256 * kPer) {
-    uint32_t k[kPer];
-    in.keys(e, k);
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      if (k[j] > top) { top = k[j]; at = e + j - in.shift; }
-      if (k[j] > kKeyNone) low = min(low, k[j]);
-    }
-  }
+  in.each(part * plan.part_len + tid * kPer, e1, 256 * kPer, [&](uint32_t k, int i) __attribute__((always_inline)) {
+    if (k > top) { top = k; at = i; }
+    low = min(low, k);
+  });
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     const uint32_t t = __shfl_xor(top, o, 64);
@@ -475,17 +482,11 @@ __global__ __launch_bounds__(256) void sample_hist_kernel(SampleArgs a, SamplePl
   const RowReader<T> in(a, row);
   const bool weigh = s.top_p < 1.0;
   const int e1 = min((part + 1) * plan.part_len, a.vocab + in.shift);
-  for (int e = part * plan.part_len + tid * kPer; e < e1; e += 256 * kPer) {
-    uint32_t k[kPer];
-    in.keys(e, k);
-#pragma unroll
-    for (int j = 0; j < kPer; ++j)
-      if (k[j] > kKeyNone) {
-        const int b = bins.of(k[j]);
-        atomicAdd(&count[b], 1u);
-        if (weigh) atomicAdd(&mass[b], fixed_of(weight_of(k[j], x.top, s.inv_t), a.shift));
-      }
-  }
+  in.each(part * plan.part_len + tid * kPer, e1, 256 * kPer, [&](uint32_t k, int) __attribute__((always_inline)) {
+    const int b = bins.of(k);
+    atomicAdd(&count[b], 1u);
+    if (weigh) atomicAdd(&mass[b], fixed_of(weight_of(k, x.top, s.inv_t), a.shift));
+  });
   __syncthreads();
   for (int b = tid; b < kBins; b += 256)
     if (count[b] != 0) {
@@ -516,22 +517,16 @@ __global__ __launch_bounds__(256) void sample_tiles_kernel(SampleArgs a, SampleP
   const int tile = part * 4 + wave, e1 = min((tile + 1) * plan.tile_len, a.vocab + in.shift);
   unsigned kept = 0;
   unsigned long long sum = 0;
-  for (int e = tile * plan.tile_len + lane * kPer; e < e1; e += 64 * kPer) {
-    uint32_t k[kPer];
-    in.keys(e, k);
-#pragma unroll
-    for (int j = 0; j < kPer; ++j)
-      if (k[j] > kKeyNone) {
-        const int b = cut ? bins.of(k[j]) : -1;
-        if (b < p_lo) {
-          const double w = weight_of(k[j], x.top, s.inv_t);
-          if (w >= s.min_p) { ++kept; sum += fixed_of(w, a.shift); }
-        } else if (b <= p_hi || b == k_bin) {
-          const unsigned at = atomicAdd(&ws.n_list, 1u);
-          if (at < kList) ws.list[at] = make_uint2(k[j], e + j - in.shift);
-        }
-      }
-  }
+  in.each(tile * plan.tile_len + lane * kPer, e1, 64 * kPer, [&](uint32_t k, int i) __attribute__((always_inline)) {
+    const int b = cut ? bins.of(k) : -1;
+    if (b < p_lo) {
+      const double w = weight_of(k, x.top, s.inv_t);
+      if (w >= s.min_p) { ++kept; sum += fixed_of(w, a.shift); }
+    } else if (b <= p_hi || b == k_bin) {
+      const unsigned at = atomicAdd(&ws.n_list, 1u);
+      if (at < kList) ws.list[at] = make_uint2(k, i);
+    }
+  });
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) { kept += __shfl_xor(kept, o, 64); sum += __shfl_xor(sum, o, 64); }
   if (lane == 0) { ws.tile_kept[tile] = kept; ws.tile_mass[tile] = sum; }
@@ -562,15 +557,17 @@ __device__ __forceinline__ unsigned long long block_before(unsigned long long v,
   return in - v;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a, SamplePlan plan, RowScratch* __restrict__ scratch) {
+// W wavefronts.
+template <typename T, int W>
+__global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, SamplePlan plan, RowScratch* __restrict__ scratch) {
   union Shared {
-    RowShared row;
+    RowShared<W> row;
     struct { unsigned long long order[kList]; unsigned long long tile[4 * kMaxParts]; } list;
   };
   __shared__ Shared sh;
-  __shared__ unsigned long long part_mass[kWaves], found_before;
-  __shared__ unsigned part_count[kWaves];
+  constexpr int kThreads = 64 * W;
+  __shared__ unsigned long long part_mass[W], found_before;
+  __shared__ unsigned part_count[W];
   __shared__ int found;
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const RowSettings s = settings_of(a, row);
@@ -596,7 +593,7 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a, Sam
       mine += k > kKeyNone;
     }
     n_list = a.vocab;
-    const unsigned finite = block_sum<kWaves>(mine, part_count);
+    const unsigned finite = block_sum<W>(mine, part_count);
     c.count_hi = finite;
     uint32_t hi = 0;
     int at = 0x7fffffff;
@@ -609,7 +606,7 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a, Sam
     __syncthreads();
     if (lane == 0) part_mass[tid >> 6] = best;
     __syncthreads();
-    for (int w = 0; w < kWaves; ++w) best = max(best, part_mass[w]);
+    for (int w = 0; w < W; ++w) best = max(best, part_mass[w]);
     top = static_cast<uint32_t>(best >> 32);
     top_idx = static_cast<int>(~static_cast<uint32_t>(best));
     __syncthreads();
@@ -627,12 +624,12 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a, Sam
   if (parts && cut) {
     whole = !bins.usable;
     if (!whole) {
-      c = find_cuts<kThreads>(scratch[row], s, a.vocab);
+      c = find_cuts<kThreads <= kBins ? kThreads : kBins>(scratch[row], s, a.vocab);
       whole = c.listed > kList;
       n_list = static_cast<int>(c.listed);
     }
     if (whole) {
-      sample_row<T>(a, row, s, top, sh.row);
+      sample_row<T, W>(a, row, s, top, sh.row);
       return;
     }
     for (int i = tid; i < n_list; i += kThreads) {
@@ -640,21 +637,43 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a, Sam
       sh.list.order[i] = (static_cast<unsigned long long>(v.x) << 32) | ~v.y;
     }
   }
-  // ---- the candidates in order: largest logit, then lowest index
+  // ---- the candidates in order: largest logit, then lowest index.  Bitonic; a list that gives a thread one candidate exchanges in a
+  // wavefront's own lanes as far as these reach, otherwise through LDS.
   int n_pow = 1;
   while (n_pow < n_list) n_pow <<= 1;
   for (int i = n_list + tid; i < n_pow; i += kThreads) sh.list.order[i] = 0ull;
   for (int i = tid; i < n_tiles; i += kThreads) sh.list.tile[i] = parts ? scratch[row].tile_mass[i] : 0ull;
   __syncthreads();
-  for (int len = 2; len <= n_pow; len <<= 1)
-    for (int half = len >> 1; half > 0; half >>= 1) {
-      for (int i = tid; i < n_pow / 2; i += kThreads) {
-        const int lo = (i / half) * 2 * half + i % half, hi = lo + half;
-        const unsigned long long u = sh.list.order[lo], v = sh.list.order[hi];
-        if ((u < v) == ((lo & len) == 0)) { sh.list.order[lo] = v; sh.list.order[hi] = u; }
+  if (n_pow <= kThreads) {
+    unsigned long long v = tid < n_pow ? sh.list.order[tid] : 0ull;
+    for (int len = 2; len <= n_pow; len <<= 1)
+      for (int half = len >> 1; half > 0; half >>= 1) {
+        unsigned long long u;
+        if (half < 64) {
+          u = __shfl_xor(v, half, 64);
+        } else {
+          __syncthreads();
+          if (tid < n_pow) sh.list.order[tid] = v;
+          __syncthreads();
+          u = tid < n_pow ? sh.list.order[tid ^ half] : 0ull;
+        }
+        const bool larger = ((tid & half) == 0) == ((tid & len) == 0);            // this place takes the larger one
+        v = larger ? (v > u ? v : u) : (v < u ? v : u);
       }
-      __syncthreads();
-    }
+    __syncthreads();
+    if (tid < n_pow) sh.list.order[tid] = v;
+    __syncthreads();
+  } else {
+    for (int len = 2; len <= n_pow; len <<= 1)
+      for (int half = len >> 1; half > 0; half >>= 1) {
+        for (int i = tid; i < n_pow / 2; i += kThreads) {
+          const int lo = (i / half) * 2 * half + i % half, hi = lo + half;
+          const unsigned long long u = sh.list.order[lo], v = sh.list.order[hi];
+          if ((u < v) == ((lo & len) == 0)) { sh.list.order[lo] = v; sh.list.order[hi] = u; }
+        }
+        __syncthreads();
+      }
+  }
   // ---- the cut among them.  This thread's are own .. own + per
   const int per = max(1, n_pow / kThreads), own = tid * per;
   auto weight_at = [&](int i) { return weight_of(static_cast<uint32_t>(sh.list.order[i] >> 32), top, s.inv_t); };
@@ -673,10 +692,10 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a, Sam
     }
     unsigned long long mass_k = 0;
     if (s.top_p < 1.0) {
-      mass_k = block_sum<kWaves>(in_k, part_mass);
+      mass_k = block_sum<W>(in_k, part_mass);
       mass_k = parts && !by_k ? c.mass_all : c.mass_k + mass_k;
     }
-    unsigned long long before = c.mass_lo + block_before<kWaves>(mine, part_mass);
+    unsigned long long before = c.mass_lo + block_before<W>(mine, part_mass);
     const double target = s.top_p * static_cast<double>(mass_k);
     unsigned kept = 0;
     for (int i = own; i < min(own + per, n_cand); ++i) {
@@ -690,14 +709,14 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a, Sam
       }
       before += f;
     }
-    kept_list = static_cast<int>(block_sum<kWaves>(kept, part_count));
+    kept_list = static_cast<int>(block_sum<W>(kept, part_count));
   }
   const unsigned long long last = kept_list > 0 ? sh.list.order[kept_list - 1] : ~0ull;     // (key, ~index) of the last kept candidate
   __syncthreads();
   // ---- the tile the number falls into
-  const unsigned long long here = tid < n_tiles ? sh.list.tile[tid] : 0ull;
-  const unsigned long long front = block_before<kWaves>(here, part_mass), total = block_sum<kWaves>(here, part_mass);
-  const unsigned n_kept = block_sum<kWaves>(parts && tid < n_tiles ? scratch[row].tile_kept[tid] : 0u, part_count) + kept_list;
+  const unsigned long long here = tid < n_tiles ? sh.list.tile[tid] : 0ull;               // (n_tiles is at most the number of threads)
+  const unsigned long long front = block_before<W>(here, part_mass), total = block_sum<W>(here, part_mass);
+  const unsigned n_kept = block_sum<W>(parts && tid < n_tiles ? scratch[row].tile_kept[tid] : 0u, part_count) + kept_list;
   const double target = s.u * static_cast<double>(total);
   if (static_cast<double>(front) <= target && static_cast<double>(front + here) > target) { found = tid; found_before = front; }
   __syncthreads();
@@ -713,7 +732,7 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a, Sam
   };
   unsigned long long sum = 0;
   for (int e = e0; e < e1; ++e) sum += fixed_of(kept_weight(e), a.shift);
-  unsigned long long before = found_before + block_before<kWaves>(sum, part_mass);
+  unsigned long long before = found_before + block_before<W>(sum, part_mass);
   if (static_cast<double>(before) <= target && static_cast<double>(before + sum) > target)
     for (int e = e0; e < e1; ++e) {
       const double w = kept_weight(e);
@@ -751,7 +770,9 @@ static void launch_sample_t(const SampleArgs& a, const SamplePlan& plan, RowScra
     if (a.top_k != nullptr || a.top_p != nullptr) hipLaunchKernelGGL(sample_hist_kernel<T>, grid, dim3(256), 0, stream, a, plan, ws);
     hipLaunchKernelGGL(sample_tiles_kernel<T>, grid, dim3(256), 0, stream, a, plan, ws);
   }
-  hipLaunchKernelGGL(sample_draw_kernel<T>, dim3(a.n_rows), dim3(kThreads), 0, stream, a, plan, ws);
+  // (behind other kernels a workgroup of four wavefronts: its barriers and sums over wavefronts are most of its time)
+  if (plan.parts > 0) hipLaunchKernelGGL((sample_draw_kernel<T, 4>), dim3(a.n_rows), dim3(256), 0, stream, a, plan, ws);
+  else hipLaunchKernelGGL((sample_draw_kernel<T, 16>), dim3(a.n_rows), dim3(1024), 0, stream, a, plan, ws);
 }
 
 void launch_sample(const void* logits, int logits_dtype, int n_rows, int vocab, long long stride, const float* temperature,
