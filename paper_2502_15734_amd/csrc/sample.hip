@@ -254,23 +254,55 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const R
   }
 }
 
+// The weights of a row in parts: 2^(y / 64) with y = (z - max z) 64 / (T ln 2), as a table of 2^(j / 64) and the series of 2^(f / 64), |f| <= 1/2, to f^5
+// (the rest is below 2^-54), times 2^shift.
+constexpr int kTable = 64;
+struct Weights {
+  double top, per, least;             // least: min_p in the same units
+  const double* table;
+  int shift;
+  // table: [kTable] in LDS, filled here by the first threads (a barrier has to follow)
+  __device__ __forceinline__ Weights(float top_logit, const RowSettings& s, int shift_, double* table_)
+      : top(top_logit), per(s.inv_t * 92.33248261689366), least(ldexp(s.min_p, shift_)), table(table_), shift(shift_) {       // 64 / ln 2
+    if (threadIdx.x < kTable) table_[threadIdx.x] = exp_of(threadIdx.x * 0.010830424696249145);       // ln 2 / 64
+  }
+  // w 2^shift; exactly 2^shift for the largest logit
+  __device__ __forceinline__ double scaled(float z) const {
+    const double y = fmax((static_cast<double>(z) - top) * per, -64.0 * 900.0), n = rint(y), f = y - n;
+    double p = 1.2417843701716925e-12;                                     // (ln 2 / 64)^5 / 5! and so on down
+    p = fma(p, f, 5.732851688640402e-10);
+    p = fma(p, f, 2.1173137155464776e-07);
+    p = fma(p, f, 5.86490495505617e-05);
+    p = fma(p, f, 0.010830424696249145);
+    p = fma(p, f, 1.0);
+    const int i = static_cast<int>(n);
+    return ldexp(table[i & (kTable - 1)] * p, (i >> 6) + shift);
+  }
+  // ... to the nearest whole number (shift <= 50: the sum with 2^52 has it in its last bits)
+  static __device__ __forceinline__ unsigned long long whole(double w) {
+    return static_cast<unsigned long long>(__double_as_longlong(w + 0x1p52) - __double_as_longlong(0x1p52));
+  }
+};
+
 // ---- a row in parts ------------------------------------------------------------------------------
-constexpr int kBins = 1024, kMaxParts = 64, kList = 4096;
+constexpr int kBins = 1024, kMaxParts = 64, kList = 4096, kLocal = 512;     // (kLocal: candidates of a part that are gathered in LDS)
 
 struct SamplePlan {
-  int parts, part_len, tile_len;      // a part is read by a workgroup, a tile (a quarter of it) by one of its wavefronts; parts 0: the list holds a row
+  int parts, part_len;                // a part is read by a workgroup, a quarter of it by a wavefront; parts 0: the list holds a row
+  int wave_tiles, tile_len;           // a wavefront's quarter has 1, 2 or 4 tiles, whose sums are kept
 };
+constexpr int kTiles = 256;           // of a row
 struct Part {
-  uint32_t top, low;                  // largest and smallest finite logit's key (low 0xffffffff: none)
+  float top, low;                     // largest and smallest logit (top -inf: none)
   int top_idx, unused;
 };
 struct RowScratch {
   Part part[kMaxParts];
   unsigned long long mass[kBins];
-  unsigned long long tile_mass[4 * kMaxParts];
+  unsigned long long tile_mass[kTiles];
   uint2 list[kList];                  // key, index
   unsigned count[kBins];
-  unsigned tile_kept[4 * kMaxParts];
+  unsigned tile_kept[kTiles];
   unsigned n_list, unused[3];
 };
 
@@ -286,8 +318,8 @@ struct RowReader {
     vocab = a.vocab;
   }
   typedef __attribute__((__vector_size__(16))) T Piece;
-  // f(key, index) for the row's elements in [e0 + lane kPer, e1) in steps of `step` elements (multiples of kPer), in the order of the indexes; kAhead
-  // pieces are loaded before the first is used.  Only the row's own logits are read, -inf and NaN passed over.
+  // f(logit, index) for the row's elements e0 .. e0 + kPer, e0 + step .., up to e1 (multiples of kPer), in the order of the indexes; kAhead pieces are
+  // loaded before the first is used.  Only the row's own logits are read; -inf and NaN are passed over.
   template <typename F>
   __device__ __forceinline__ void each(int e0, int e1, int step, F&& f) const {
     constexpr int kAhead = 4;
@@ -306,8 +338,8 @@ struct RowReader {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
           if (!whole && (i + j < 0 || i + j >= vocab)) continue;
-          const uint32_t k = logit_key(to_float(whole ? v[a][j] : row[i + j]));
-          if (k > kKeyNone) f(k, i + j);
+          const float z = to_float(whole ? v[a][j] : row[i + j]);
+          if (z > -INFINITY) f(z, i + j);
         }
       }
     }
@@ -315,16 +347,17 @@ struct RowReader {
 };
 
 // The row's extremes from its parts: every wavefront for itself.
+__device__ __forceinline__ bool ahead(float z, int i, float than, int than_i) { return z > than || (z == than && i < than_i); }
 __device__ __forceinline__ Part row_extremes(const RowScratch& ws, int parts) {
   const int lane = threadIdx.x & 63;
-  Part p{0, 0xffffffffu, 0x7fffffff, 0};
+  Part p{-INFINITY, INFINITY, 0x7fffffff, 0};
   if (lane < parts) p = ws.part[lane];
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
-    const uint32_t top = __shfl_xor(p.top, o, 64), low = __shfl_xor(p.low, o, 64);
+    const float top = __shfl_xor(p.top, o, 64), low = __shfl_xor(p.low, o, 64);
     const int idx = __shfl_xor(p.top_idx, o, 64);
-    if (top > p.top || (top == p.top && idx < p.top_idx)) { p.top = top; p.top_idx = idx; }
-    p.low = min(p.low, low);
+    if (ahead(top, idx, p.top, p.top_idx)) { p.top = top; p.top_idx = idx; }
+    p.low = fminf(p.low, low);
   }
   return p;
 }
@@ -333,14 +366,13 @@ __device__ __forceinline__ Part row_extremes(const RowScratch& ws, int parts) {
 // the bins are in that order and equal logits share one.
 struct Bins {
   float top, per;
-  bool usable;                        // not beside +inf
-  __device__ __forceinline__ Bins(uint32_t top_key, uint32_t low_key, double inv_t) {
-    top = logit_of(top_key);
-    const float span = fminf(top - logit_of(low_key), static_cast<float>(46.0 / inv_t));
+  bool usable;
+  __device__ __forceinline__ Bins(float top_, float low, double inv_t) : top(top_) {
+    const float span = fminf(top - low, static_cast<float>(46.0 / inv_t));
     per = span > 0.f ? kBins / span : 0.f;
-    usable = top_key != kKeyInf && span < INFINITY && per < INFINITY;
+    usable = span < INFINITY && per < INFINITY;
   }
-  __device__ __forceinline__ int of(uint32_t key) const { return static_cast<int>(fminf((top - logit_of(key)) * per, static_cast<float>(kBins - 1))); }
+  __device__ __forceinline__ int of(float z) const { return static_cast<int>(fminf((top - z) * per, static_cast<float>(kBins - 1))); }
 };
 
 struct Cuts {
@@ -437,19 +469,19 @@ __global__ __launch_bounds__(256) void sample_max_kernel(SampleArgs a, SamplePla
   const RowReader<T> in(a, row);
   for (int b = part * 256 + tid; b < kBins; b += plan.parts * 256) { ws.count[b] = 0; ws.mass[b] = 0; }
   if (part == 0 && tid == 0) ws.n_list = 0;
-  uint32_t top = 0, low = 0xffffffffu;
+  float top = -INFINITY, low = INFINITY;
   int at = 0x7fffffff;
   const int e1 = min((part + 1) * plan.part_len, a.vocab + in.shift);
-  in.each(part * plan.part_len + tid * kPer, e1, 256 * kPer, [&](uint32_t k, int i) __attribute__((always_inline)) {
-    if (k > top) { top = k; at = i; }
-    low = min(low, k);
+  in.each(part * plan.part_len + tid * kPer, e1, 256 * kPer, [&](float z, int i) __attribute__((always_inline)) {
+    if (z > top) { top = z; at = i; }
+    low = fminf(low, z);
   });
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
-    const uint32_t t = __shfl_xor(top, o, 64);
+    const float t = __shfl_xor(top, o, 64);
     const int i = __shfl_xor(at, o, 64);
-    if (t > top || (t == top && i < at)) { top = t; at = i; }
-    low = min(low, static_cast<uint32_t>(__shfl_xor(low, o, 64)));
+    if (ahead(t, i, top, at)) { top = t; at = i; }
+    low = fminf(low, __shfl_xor(low, o, 64));
   }
   if (lane == 0) wave_part[wave] = Part{top, low, at, 0};
   __syncthreads();
@@ -457,8 +489,8 @@ __global__ __launch_bounds__(256) void sample_max_kernel(SampleArgs a, SamplePla
     Part p = wave_part[0];
     for (int w = 1; w < 4; ++w) {
       const Part o = wave_part[w];
-      if (o.top > p.top || (o.top == p.top && o.top_idx < p.top_idx)) { p.top = o.top; p.top_idx = o.top_idx; }
-      p.low = min(p.low, o.low);
+      if (ahead(o.top, o.top_idx, p.top, p.top_idx)) { p.top = o.top; p.top_idx = o.top_idx; }
+      p.low = fminf(p.low, o.low);
     }
     ws.part[part] = p;
   }
@@ -469,23 +501,24 @@ __global__ __launch_bounds__(256) void sample_hist_kernel(SampleArgs a, SamplePl
   constexpr int kPer = RowReader<T>::kPer;
   __shared__ unsigned count[kBins];
   __shared__ unsigned long long mass[kBins];
+  __shared__ double table[kTable];
   const int part = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
   RowScratch& ws = scratch[row];
   const RowSettings s = settings_of(a, row);
   if (s.greedy || !needs_cut(a, s)) return;
   const Part x = row_extremes(ws, plan.parts);
-  if (x.top <= kKeyNone) return;
   const Bins bins(x.top, x.low, s.inv_t);
-  if (!bins.usable) return;
+  if (!(fabsf(x.top) < INFINITY) || !bins.usable) return;
+  const Weights weights(x.top, s, a.shift, table);
   for (int b = tid; b < kBins; b += 256) { count[b] = 0; mass[b] = 0; }
   __syncthreads();
   const RowReader<T> in(a, row);
   const bool weigh = s.top_p < 1.0;
   const int e1 = min((part + 1) * plan.part_len, a.vocab + in.shift);
-  in.each(part * plan.part_len + tid * kPer, e1, 256 * kPer, [&](uint32_t k, int) __attribute__((always_inline)) {
-    const int b = bins.of(k);
+  in.each(part * plan.part_len + tid * kPer, e1, 256 * kPer, [&](float z, int) __attribute__((always_inline)) {
+    const int b = bins.of(z);
     atomicAdd(&count[b], 1u);
-    if (weigh) atomicAdd(&mass[b], fixed_of(weight_of(k, x.top, s.inv_t), a.shift));
+    if (weigh) atomicAdd(&mass[b], Weights::whole(weights.scaled(z)));
   });
   __syncthreads();
   for (int b = tid; b < kBins; b += 256)
@@ -498,15 +531,20 @@ __global__ __launch_bounds__(256) void sample_hist_kernel(SampleArgs a, SamplePl
 template <typename T>
 __global__ __launch_bounds__(256) void sample_tiles_kernel(SampleArgs a, SamplePlan plan, RowScratch* __restrict__ scratch) {
   constexpr int kPer = RowReader<T>::kPer;
+  __shared__ double table[kTable];
+  __shared__ uint2 list[kLocal];                       // the part's candidates: a place in the row's list for each would be a trip to memory in the loop
+  __shared__ unsigned n_list, first;
   const int part = blockIdx.x, row = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   RowScratch& ws = scratch[row];
   const RowSettings s = settings_of(a, row);
   if (s.greedy) return;
+  if (tid == 0) n_list = 0;
   const Part x = row_extremes(ws, plan.parts);
-  if (x.top <= kKeyNone) return;
   const Bins bins(x.top, x.low, s.inv_t);
   const bool cut = needs_cut(a, s);
-  if (cut && !bins.usable) return;
+  if (!(fabsf(x.top) < INFINITY) || (cut && !bins.usable)) return;
+  const Weights weights(x.top, s, a.shift, table);
+  __syncthreads();
   int p_lo = kBins, p_hi = kBins, k_bin = kBins;
   if (cut) {
     const Cuts c = find_cuts<256>(ws, s, a.vocab);
@@ -514,22 +552,45 @@ __global__ __launch_bounds__(256) void sample_tiles_kernel(SampleArgs a, SampleP
     p_lo = c.p_lo; p_hi = c.p_hi; k_bin = c.k_bin;
   }
   const RowReader<T> in(a, row);
-  const int tile = part * 4 + wave, e1 = min((tile + 1) * plan.tile_len, a.vocab + in.shift);
-  unsigned kept = 0;
-  unsigned long long sum = 0;
-  in.each(tile * plan.tile_len + lane * kPer, e1, 64 * kPer, [&](uint32_t k, int i) __attribute__((always_inline)) {
-    const int b = cut ? bins.of(k) : -1;
-    if (b < p_lo) {
-      const double w = weight_of(k, x.top, s.inv_t);
-      if (w >= s.min_p) { ++kept; sum += fixed_of(w, a.shift); }
-    } else if (b <= p_hi || b == k_bin) {
-      const unsigned at = atomicAdd(&ws.n_list, 1u);
-      if (at < kList) ws.list[at] = make_uint2(k, i);
-    }
-  });
+  const int tile0 = (part * 4 + wave) * plan.wave_tiles;
+  unsigned kept[4] = {0, 0, 0, 0};
+  unsigned long long sum[4] = {0, 0, 0, 0};
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) { kept += __shfl_xor(kept, o, 64); sum += __shfl_xor(sum, o, 64); }
-  if (lane == 0) { ws.tile_kept[tile] = kept; ws.tile_mass[tile] = sum; }
+  for (int t = 0; t < 4; ++t)
+    if (t < plan.wave_tiles) {
+      const int e0 = (tile0 + t) * plan.tile_len;
+      in.each(e0 + lane * kPer, min(e0 + plan.tile_len, a.vocab + in.shift), 64 * kPer, [&](float z, int i) __attribute__((always_inline)) {
+        const int b = cut ? bins.of(z) : -1;
+        if (b < p_lo) {
+          const double w = weights.scaled(z);
+          if (w >= weights.least) { ++kept[t]; sum[t] += Weights::whole(w); }
+        } else if (b <= p_hi || b == k_bin) {
+          const unsigned at = atomicAdd(&n_list, 1u);
+          if (at < kLocal) {
+            list[at] = make_uint2(logit_key(z), i);
+          } else {
+            const unsigned to = atomicAdd(&ws.n_list, 1u);
+            if (to < kList) ws.list[to] = make_uint2(logit_key(z), i);
+          }
+        }
+      });
+    }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (t < plan.wave_tiles) { kept[t] += __shfl_xor(kept[t], o, 64); sum[t] += __shfl_xor(sum[t], o, 64); }
+  if (lane == 0)
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (t < plan.wave_tiles) { ws.tile_kept[tile0 + t] = kept[t]; ws.tile_mass[tile0 + t] = sum[t]; }
+  __syncthreads();
+  const unsigned n = min(n_list, static_cast<unsigned>(kLocal));
+  if (n == 0) return;
+  if (tid == 0) first = atomicAdd(&ws.n_list, n);
+  __syncthreads();
+  for (unsigned i = tid; i < n; i += 256)
+    if (first + i < kList) ws.list[first + i] = list[i];
 }
 
 template <int N, typename V>
@@ -562,18 +623,19 @@ template <typename T, int W>
 __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, SamplePlan plan, RowScratch* __restrict__ scratch) {
   union Shared {
     RowShared<W> row;
-    struct { unsigned long long order[kList]; unsigned long long tile[4 * kMaxParts]; } list;
+    struct { unsigned long long order[kList]; unsigned long long tile[kTiles]; } list;
   };
   __shared__ Shared sh;
   constexpr int kThreads = 64 * W;
   __shared__ unsigned long long part_mass[W], found_before;
   __shared__ unsigned part_count[W];
   __shared__ int found;
+  __shared__ double table[kTable];
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const RowSettings s = settings_of(a, row);
   const bool parts = plan.parts > 0, cut = !parts || needs_cut(a, s);
   const RowReader<T> in(a, row);
-  const int tile_len = parts ? plan.tile_len : kList, shift = parts ? in.shift : 0, n_tiles = parts ? 4 * plan.parts : 1;
+  const int tile_len = parts ? plan.tile_len : kList, shift = parts ? in.shift : 0, n_tiles = parts ? 4 * plan.wave_tiles * plan.parts : 1;
   uint32_t top;
   int top_idx;
   Part x{0, 0, 0, 0};
@@ -582,7 +644,7 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
   bool whole = false;                                  // the list does not hold the candidates
   if (parts) {
     x = row_extremes(scratch[row], plan.parts);
-    top = x.top;
+    top = logit_key(x.top);
     top_idx = x.top_idx;
   } else {
     // the whole row is the list: (key, ~index), nothing behind it
@@ -620,22 +682,24 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
     }
     return;
   }
-  const Bins bins(top, parts ? x.low : top, s.inv_t);
-  if (parts && cut) {
-    whole = !bins.usable;
-    if (!whole) {
-      c = find_cuts<kThreads <= kBins ? kThreads : kBins>(scratch[row], s, a.vocab);
-      whole = c.listed > kList;
-      n_list = static_cast<int>(c.listed);
-    }
-    if (whole) {
-      sample_row<T, W>(a, row, s, top, sh.row);
-      return;
-    }
-    for (int i = tid; i < n_list; i += kThreads) {
-      const uint2 v = scratch[row].list[i];
-      sh.list.order[i] = (static_cast<unsigned long long>(v.x) << 32) | ~v.y;
-    }
+  const float top_logit = logit_of(top);
+  const Bins bins(top_logit, parts ? x.low : top_logit, s.inv_t);
+  whole = top == kKeyInf || (parts && cut && !bins.usable);
+  const Weights weights(top_logit, s, a.shift, table);
+  __syncthreads();
+  if (!whole && parts && cut) {
+    c = find_cuts<kThreads>(scratch[row], s, a.vocab);
+    whole = c.listed > kList;
+    n_list = static_cast<int>(c.listed);
+    if (!whole)
+      for (int i = tid; i < n_list; i += kThreads) {
+        const uint2 v = scratch[row].list[i];
+        sh.list.order[i] = (static_cast<unsigned long long>(v.x) << 32) | ~v.y;
+      }
+  }
+  if (whole) {
+    sample_row<T, W>(a, row, s, top, sh.row);
+    return;
   }
   // ---- the candidates in order: largest logit, then lowest index.  Bitonic; a list that gives a thread one candidate exchanges in a
   // wavefront's own lanes as far as these reach, otherwise through LDS.
@@ -676,7 +740,7 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
   }
   // ---- the cut among them.  This thread's are own .. own + per
   const int per = max(1, n_pow / kThreads), own = tid * per;
-  auto weight_at = [&](int i) { return weight_of(static_cast<uint32_t>(sh.list.order[i] >> 32), top, s.inv_t); };
+  auto weight_at = [&](int i) { return weights.scaled(logit_of(static_cast<uint32_t>(sh.list.order[i] >> 32))); };
   int n_cand = n_list, kept_list = 0;
   if (!parts) n_cand = static_cast<int>(c.count_hi);
   if (cut) {
@@ -686,7 +750,7 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
     const int n_k = by_k ? base_k + s.top_k - static_cast<int>(c.count_k) : n_cand;
     unsigned long long in_k = 0, mine = 0;
     for (int i = own; i < min(own + per, n_cand); ++i) {
-      const unsigned long long w = fixed_of(weight_at(i), a.shift);
+      const unsigned long long w = Weights::whole(weight_at(i));
       mine += w;
       if (i >= base_k && i < n_k) in_k += w;
     }
@@ -700,9 +764,9 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
     unsigned kept = 0;
     for (int i = own; i < min(own + per, n_cand); ++i) {
       const double w = weight_at(i);
-      const unsigned long long f = fixed_of(w, a.shift);
+      const unsigned long long f = Weights::whole(w);
       const bool first = i == 0 && c.p_lo == 0;        // rank 0
-      if (first || (i < n_k && (s.top_p >= 1.0 || static_cast<double>(before) < target) && w >= s.min_p)) {
+      if (first || (i < n_k && (s.top_p >= 1.0 || static_cast<double>(before) < target) && w >= weights.least)) {
         ++kept;
         const int e = static_cast<int>(~static_cast<uint32_t>(sh.list.order[i])) + shift;
         atomicAdd(&sh.list.tile[e / tile_len], f);
@@ -724,22 +788,22 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
   auto kept_weight = [&](int e) {
     const int i = e - shift;
     if (i < 0) return 0.0;
-    const uint32_t k = key_at<T>(a, row, i);
-    if (k <= kKeyNone) return 0.0;
-    if (cut && !(parts && bins.of(k) < c.p_lo) && ((static_cast<unsigned long long>(k) << 32) | ~static_cast<uint32_t>(i)) < last) return 0.0;
-    const double w = weight_of(k, top, s.inv_t);
-    return w >= s.min_p ? w : 0.0;
+    const float z = to_float(in.row[i]);
+    if (!(z > -INFINITY)) return 0.0;
+    if (cut && !(parts && bins.of(z) < c.p_lo) && ((static_cast<unsigned long long>(logit_key(z)) << 32) | ~static_cast<uint32_t>(i)) < last) return 0.0;
+    const double w = weights.scaled(z);
+    return w >= weights.least ? w : 0.0;
   };
   unsigned long long sum = 0;
-  for (int e = e0; e < e1; ++e) sum += fixed_of(kept_weight(e), a.shift);
+  for (int e = e0; e < e1; ++e) sum += Weights::whole(kept_weight(e));
   unsigned long long before = found_before + block_before<W>(sum, part_mass);
   if (static_cast<double>(before) <= target && static_cast<double>(before + sum) > target)
     for (int e = e0; e < e1; ++e) {
       const double w = kept_weight(e);
-      before += fixed_of(w, a.shift);
+      before += Weights::whole(w);
       if (static_cast<double>(before) > target) {
         a.token[row] = e - shift;
-        if (a.logprob != nullptr) a.logprob[row] = static_cast<float>(log(w / ldexp(static_cast<double>(total), -a.shift)));
+        if (a.logprob != nullptr) a.logprob[row] = static_cast<float>(log(w / static_cast<double>(total)));
         if (a.n_kept != nullptr) a.n_kept[row] = static_cast<int>(n_kept);
         break;
       }
@@ -748,13 +812,15 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
 
 // Parts of at least 2048 logits, so many that a call has about a thousand workgroups (four on a compute unit), at most 64 a row.
 SamplePlan sample_plan(int n_rows, int vocab) {
-  SamplePlan p{0, 0, 0};
+  SamplePlan p{0, 0, 0, 0};
   if (vocab <= kList) return p;
   const long long wanted = std::max(1, std::min(kMaxParts, 1024 / std::max(1, n_rows)));
   const long long len = std::max((vocab + 8 + wanted - 1) / wanted, 2048ll);      // (8: a row's beginning inside a piece)
   p.part_len = static_cast<int>((len + 2047) / 2048 * 2048);
-  p.tile_len = p.part_len / 4;
   p.parts = (vocab + 8 + p.part_len - 1) / p.part_len;
+  // (tiles of 1024 logits and more: what the last kernel reads of the row once more is a tile)
+  p.wave_tiles = p.parts <= kTiles / 16 && p.part_len >= 16384 ? 4 : p.parts <= kTiles / 8 && p.part_len >= 8192 ? 2 : 1;
+  p.tile_len = p.part_len / (4 * p.wave_tiles);
   return p;
 }
 
