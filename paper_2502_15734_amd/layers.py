@@ -10,6 +10,8 @@ hook.
 DecoderLoop (whole layers): the hidden states of the chosen rows pass through normalisation,
 projections, the partial prefill and the feed-forward network of every layer.
 
+AnswerLoop: the answers behind a DecoderLoop's prefill, token by token over the pages it left.
+
 Argument marshalling and call order only; every step runs in libcachecraft.
 """
 from __future__ import annotations
@@ -35,13 +37,20 @@ class DecoderLoop:
     other chunks leave the list (Sec. 3.2.2) and the surviving rows' hidden states are compacted."""
 
     def __init__(self, w, weights: Sequence, window: Optional[int] = None, impl: int = CC_IMPL_AUTO,
-                 device: str = "cuda", preload: bool = False, depth: int = 1):
+                 device: str = "cuda", preload: bool = False, depth: int = 1, answer_tokens: int = 0):
         """preload: every layer's chunk store comes from pinned host memory through the layer-wise
-        preloader (Algorithm 2), `depth` layers ahead of the one being computed."""
+        preloader (Algorithm 2), `depth` layers ahead of the one being computed.
+        answer_tokens: if given, every layer keeps request pages of its own, with room for that many more tokens
+        of each request, so that an AnswerLoop can go on from them (not with preload, whose slots hold the
+        values of later layers by then)."""
         assert w.hidden is not None, "the workload must carry hidden states"
-        self.w, self.window = w, window
-        self.batch = DeviceBatch(w, device=device, impl=impl)
+        assert not (preload and answer_tokens), "the preloader's slots do not keep a layer's values for the answer"
+        self.w, self.window, self.answer_tokens = w, window, answer_tokens
+        spare = w.n_requests * ((answer_tokens + 15) // 16 + 1) if answer_tokens else 0
+        self.batch = DeviceBatch(w, device=device, impl=impl, spare_blocks=spare)
         b = self.batch
+        self.pages = [(b.k_req, b.v_req, b.v_map)] + [(b.k_req.clone(), b.v_req.clone(), b.v_map.clone())
+                                                      for _ in weights[1:]] if answer_tokens else []
         up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(device).to(b.dt)
         self.weights = [{k: up(getattr(lw, k)) for k in ("gain_attn", "gain_ffn", "w_qkv", "w_o", "w_gate", "w_up", "w_down")}
                         for lw in weights]
@@ -75,6 +84,8 @@ class DecoderLoop:
     def _shift(self, l):
         """Layer l's chunk-caches (waiting for the preloader's copy if there is one), re-positioned."""
         b = self.batch
+        if self.pages:
+            b.k_req, b.v_req, b.v_map = self.pages[l]
         if self.pre is not None:
             self.pre[0].acquire(l); self.pre[1].acquire(l)
             b.k_store, b.v_store = self.slots[l % len(self.slots)]
@@ -172,6 +183,139 @@ class DecoderLoop:
             for p in self.pre:
                 p.close()
             self.pre = None
+
+
+class AnswerLoop:
+    """Answers behind a DecoderLoop's prefill (made with answer_tokens), one token per request and step: cc_sample from the last row's logits ->
+    cc_extend_segments (a token more per request) -> the token's embedding -> per layer cc_rms_norm -> cc_qkv_project ->
+    cc_append_attention over the layer's pages -> cc_linear -> cc_rms_norm -> cc_gated_linear -> cc_linear, -> logits.
+    embed [vocab, hidden], gain_out [hidden], w_out [vocab, hidden]: embedding, last normalisation, output projection (numpy).
+    temperature, top_k, top_p, min_p: one value, or one per request; None: off.  stop: a request that draws this token
+    gets no further one.  Nothing of a step depends on the host, so graph=True captures one and replays it."""
+
+    def __init__(self, loop: DecoderLoop, embed, gain_out, w_out, eps: float = 1.0e-5, temperature=None, top_k=None, top_p=None,
+                 min_p=None, stop: Optional[int] = None):
+        assert loop.answer_tokens > 0, "the DecoderLoop must keep its pages (answer_tokens)"
+        self.loop, self.eps, self.stop = loop, float(eps), stop
+        w, b = loop.w, loop.batch
+        self.b, self.n = b, w.n_requests
+        dev = b.device
+        up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(dev).to(b.dt)
+        self.embed, self.gain_out, self.w_out = up(embed), up(gain_out), up(w_out)
+        n, hidden, vocab = self.n, self.embed.shape[1], self.w_out.shape[0]
+        ffn = loop.weights[0]["w_gate"].shape[0]
+        hq, hkv, d = w.spec.n_q_heads, w.spec.n_kv_heads, w.spec.head_dim
+        # tables: every request's last segment moves to a place with room for the answer, its pages stay
+        seg, last = np.array(w.segments, copy=True), np.asarray(w.req_seg_off[1:]) - 1
+        assert (np.diff(w.req_seg_off) > 0).all() and (seg[last, 1] == 1).all(), "every request needs a question, behind which the answer comes"
+        pages = lambda t: (t + 15) // 16
+        cap = pages(seg[:, 3])
+        tab = [np.asarray(w.req_tab)]
+        at = len(w.req_tab)
+        for s in last:
+            held, room = int(cap[s]), int(pages(seg[s, 3] + loop.answer_tokens))
+            tab.append(np.concatenate([w.req_tab[seg[s, 4]: seg[s, 4] + held], np.full(room - held, -1)]))
+            seg[s, 4], cap[s] = at, room
+            at += room
+        i32 = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(dev)
+        self.segs, self.tab_cap, self.block_tab = i32(seg), i32(cap), i32(np.concatenate(tab))
+        self.free = i32(np.arange(w.n_req_blocks, b.k_req.shape[0]))
+        self.free_left = self.free.clone()
+        self.last_seg = torch.from_numpy(last.astype(np.int64)).to(dev)
+        self.n_new = i32(np.zeros(len(seg)))
+        self.cu_q, self.counts = i32(np.zeros(n + 1)), i32(np.zeros(4))
+        self.q_pos, self.slot_map, self.row_req, self.last_row, self.status = (i32(np.zeros(n)) for _ in range(5))
+        self.max_ctx = max(w.context_len(r) for r in range(n)) + loop.answer_tokens
+        self.max_segs = int(np.diff(w.req_seg_off).max())
+        # rows of a step
+        mk = lambda cols: torch.zeros((n, cols), dtype=b.dt, device=dev)
+        self.h, self.h1, self.x, self.act, self.h_last, self.logits = mk(hidden), mk(hidden), mk(hidden), mk(ffn), mk(hidden), mk(vocab)
+        self.q, self.k, self.v, self.o = (torch.zeros((n, heads, d), dtype=b.dt, device=dev) for heads in (hq, hkv, hkv, hq))
+        ctx = b.ctx
+        self.ws_products = product_workspace(n, dev, lambda r: ctx.qkv_project_workspace_bytes(r, hidden),
+                                             lambda r: ctx.linear_workspace_bytes(r, hq * d, hidden), lambda r: ctx.linear_workspace_bytes(r, ffn, hidden),
+                                             lambda r: ctx.linear_workspace_bytes(r, hidden, vocab))
+        self.ws = torch.empty(max(256, ctx.extend_segments_workspace_bytes(len(seg), n), ctx.sample_workspace_bytes(n, vocab),
+                                  ctx.append_attention_workspace_bytes(n, 1, n, self.max_ctx, self.max_segs)), dtype=torch.uint8, device=dev)
+        one = lambda a, t: None if a is None else torch.as_tensor(np.broadcast_to(np.asarray(a, dtype=t), (n,)).copy()).to(dev)
+        self.settings = dict(temperature=one(temperature, np.float32), top_k=one(top_k, np.int32), top_p=one(top_p, np.float32),
+                             min_p=one(min_p, np.float32))
+        self.u = torch.zeros(n, dtype=torch.float32, device=dev)
+        self.token, self.n_kept = i32(np.zeros(n)), i32(np.zeros(n))
+        self.logprob = torch.zeros(n, dtype=torch.float32, device=dev)
+        self.alive = torch.ones(n, dtype=torch.bool, device=dev)
+        self.drawn = 0                                                 # tokens drawn; all but the last have been through the layers
+        self.h_last.copy_(loop.h[b.cu_q[1:].long() - 1])               # the prefill's last row of every request
+        self._logits()
+
+    def _logits(self):
+        c = self.b.ctx
+        c.rms_norm(self.h_last, self.gain_out, self.eps, self.x)
+        c.linear(self.x, self.w_out, self.logits, workspace=self.ws_products)
+
+    def _draw(self):
+        """The next token of every request from the logits; -1 for those that have stopped."""
+        self.b.ctx.sample(self.logits, self.logits.shape[1], self.u, self.token, logprob=self.logprob, n_kept=self.n_kept, workspace=self.ws,
+                          **self.settings)
+        self.token.masked_fill_(~self.alive, -1)
+        if self.stop is not None:
+            self.alive &= self.token != self.stop
+
+    def _feed(self):
+        """The drawn tokens through the layers."""
+        b, c = self.b, self.b.ctx
+        self.n_new.index_copy_(0, self.last_seg, self.alive.int())
+        c.extend_segments(self.segs, self.n_new, self.tab_cap, b.req_seg_off, self.free_left, self.block_tab, b.k_req.shape[0], self.segs, self.cu_q,
+                          self.q_pos, self.slot_map, self.row_req, self.last_row, self.status, self.counts, self.ws)
+        # (the pages taken leave the list: what is left moves to its front, the end repeats its last entry and is never reached)
+        left = torch.arange(self.free.shape[0], device=self.free.device) + self.counts[1]
+        self.free_left.copy_(self.free_left[left.clamp(max=self.free.shape[0] - 1)])
+        rows = self.token[self.row_req.long().clamp(min=0)].masked_fill(self.row_req < 0, -1)
+        c.gather_rows(self.embed, rows, self.h)
+        for l, lw in enumerate(self.loop.weights):
+            k_pool, v_pool, v_map = self.loop.pages[l]
+            c.rms_norm(self.h, lw["gain_attn"], self.loop.eps[l], self.x)
+            c.qkv_project(self.x, lw["w_qkv"], self.q, self.k, self.v, workspace=self.ws_products)
+            c.append_attention(self.q, self.k, self.v, self.q_pos, self.slot_map, self.cu_q, 1, k_pool, v_pool, self.block_tab, self.segs,
+                               b.req_seg_off, self.n, self.max_ctx, self.max_segs, self.o, None, self.ws,
+                               shared=(b.v_store, v_map) if b.cow else None)
+            c.linear(self.o.view(self.n, -1), lw["w_o"], self.h1, residual=self.h, workspace=self.ws_products)
+            c.rms_norm(self.h1, lw["gain_ffn"], self.loop.eps[l], self.x)
+            c.gated_linear(self.x, lw["w_gate"], lw["w_up"], self.act)
+            c.linear(self.act, lw["w_down"], self.h, residual=self.h1, workspace=self.ws_products)
+        c.gather_rows(self.h, self.last_row, self.h_last)
+        self._logits()
+
+    def run(self, u, graph: bool = False, keep: bool = False):
+        """u [steps, requests]: the uniform numbers the tokens are drawn with (at most answer_tokens + 1 steps in all).  Returns the tokens [steps,
+        requests] (-1: none) and their log-probabilities; with keep also the logits each was drawn from."""
+        u = torch.as_tensor(np.ascontiguousarray(u, dtype=np.float32)).to(self.u.device)
+        if self.drawn + u.shape[0] > self.loop.answer_tokens + 1:
+            raise ValueError("AnswerLoop: more tokens than the pages have room for")
+        tokens, logprobs, logits, captured, fed = [], [], [], None, False
+        for step in range(u.shape[0]):
+            if self.drawn == 0:
+                pass                                                  # (the prefill's logits)
+            elif captured is not None:
+                captured.replay()
+            else:
+                self._feed()
+                if graph and fed:                                     # (the second eager step: lazy set-up stays out of the graph)
+                    torch.cuda.synchronize()
+                    captured = torch.cuda.CUDAGraph()
+                    with torch.cuda.graph(captured):
+                        self._feed()
+                fed = True
+            self.u.copy_(u[step])
+            if keep:
+                logits.append(self.logits.float().cpu().numpy())
+            self._draw()
+            self.drawn += 1
+            tokens.append(self.token.clone())
+            logprobs.append(self.logprob.clone())
+        torch.cuda.synchronize()
+        out = torch.stack(tokens).cpu().numpy(), torch.stack(logprobs).cpu().numpy()
+        return out + (logits,) if keep else out
 
 
 class LayerLoop:

@@ -29,8 +29,9 @@ def product_workspace(n_rows: int, device, *needs) -> torch.Tensor:
 
 class DeviceBatch:
     def __init__(self, w, device: str = "cuda", impl: int = CC_IMPL_AUTO, poison: bool = False,
-                 miss_segments=(), fused_gather: bool = True, cow: bool = True):
-        """cow: values of cached chunks stay in the store (cc_rope_shift only records where they are);
+                 miss_segments=(), fused_gather: bool = True, cow: bool = True, spare_blocks: int = 0):
+        """spare_blocks: blocks of the request pool behind those the prompts own, for tokens that come later.
+        cow: values of cached chunks stay in the store (cc_rope_shift only records where they are);
         cc_sparse_prefill copies a page's values into the request's pool when it recomputes one of its
         tokens and reads all the others from the store (cc_shared_values).
         miss_segments: global indices of chunk segments that have NO chunk-cache in this batch: they
@@ -50,7 +51,7 @@ class DeviceBatch:
         # shared chunk store (read-only) and request-owned pages
         self.k_store = _dev(w.k_store, dt, device)
         self.v_store = _dev(w.v_store, dt, device)
-        nb = max(1, w.n_req_blocks)
+        nb = max(1, w.n_req_blocks + spare_blocks)
         fill = float("nan") if poison else 0.0
         self.k_req = torch.full((nb, hkv, 16, d), fill, dtype=dt, device=device)
         self.v_req = torch.full((nb, hkv, d, 16), fill, dtype=dt, device=device)

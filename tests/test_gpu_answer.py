@@ -536,3 +536,114 @@ def test_sample_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         _check_sample(o, z, vocab, draw, **settings)
+
+
+# ---- all of them: answers behind a prefill -------------------------------------------------------------------------------------
+def _answer_setup(dtype, n_layers=2, answer=20, window=None, vocab=None, **settings):
+    import workload as W
+    from paper_2502_15734_amd.layers import AnswerLoop, DecoderLoop
+    hq, hkv, d = (8, 2, 128) if dtype == "bf16" else (4, 2, 64)
+    reqs = [W.RequestSpec([0, 1, 2], [0.3, 0.2, 0.25], 21), W.RequestSpec([2, 0], [0.5, 0.15], 16), W.RequestSpec([1], [0.2], 3)]
+    w = W.custom("answer", dtype, hq, hkv, d, THETA, [100, 77, 64], [0, 5, 0], reqs, 1.0 / math.sqrt(d), seed=53, hidden=256)
+    ffn, vocab = (640 if dtype == "bf16" else 160), vocab or (640 if dtype == "bf16" else 611)
+    weights = [W.layer_weights(w.spec, 256, ffn, layer=l, qkv_scale=1.0 / 16) for l in range(n_layers)]
+    rng = np.random.default_rng(7)
+    rnd = W.round_to_bf16 if dtype == "bf16" else (lambda a: a)
+    embed = rnd(rng.standard_normal((vocab, 256)).astype(np.float32))
+    w_out = rnd((rng.standard_normal((vocab, 256)) / 4).astype(np.float32))
+    gain = rnd(np.float32(1.0) + 0.1 * rng.standard_normal(256).astype(np.float32))
+    loop = DecoderLoop(w, weights, window=window, answer_tokens=answer)
+    loop.run()
+    before = [(k.float().cpu().numpy(), v.float().cpu().numpy(), m.cpu().numpy()) for k, v, m in loop.pages]
+    ans = AnswerLoop(loop, embed, gain, w_out, **settings)
+    return w, weights, loop, ans, before, (embed, gain, w_out)
+
+
+def _oracle_answer(w, weights, ans, before, model, tokens, eps=1.0e-5):
+    """Logits in front of every token, in 64 bits, of answers that go `tokens` [steps, requests], from the pages and hidden states the prefill left."""
+    from oracle import cachecraft_oracle as O
+    embed, gain, w_out = (np.asarray(a, np.float64) for a in model)
+    hq, hkv, d = w.spec.n_q_heads, w.spec.n_kv_heads, w.spec.head_dim
+    store = ans.b.v_store.float().cpu().numpy()
+    out = [[] for _ in tokens]
+    last = ans.loop.h[ans.b.cu_q[1:].long() - 1].double().cpu().numpy()
+    for r in range(w.n_requests):
+        caches = []
+        for k, v, m in before:
+            caches.append(list(A.paged_context(k, v, lambda p: store[m[p]] if m[p] >= 0 else v[p], w.req_tab, w.segments, range(w.req_seg_off[r], w.req_seg_off[r + 1]))))
+        h = last[r:r + 1]
+        for step in range(len(tokens)):
+            if step:
+                h = embed[tokens[step - 1][r]][None]
+                for lw, cache in zip(weights, caches):
+                    x = O.rms_norm(h, lw.gain_attn, lw.eps)
+                    qkv = x @ np.asarray(lw.w_qkv, np.float64).T
+                    q, kn, vn = qkv[:, :hq * d].reshape(1, hq, d), qkv[:, hq * d:(hq + hkv) * d].reshape(1, hkv, d), qkv[:, (hq + hkv) * d:].reshape(1, hkv, d)
+                    p = len(cache[0])
+                    cache[0], cache[1], cache[2] = np.append(cache[0], p), np.concatenate([cache[1], A.rotate(kn, [p], THETA)]), np.concatenate([cache[2], vn])
+                    o = A.attend(q, np.array([p]), *cache, THETA, 0.0)[0].reshape(1, -1)
+                    h1 = h + O.linear(o, lw.w_o)
+                    h = h1 + O.linear(O.gated_ffn_in(O.rms_norm(h1, lw.gain_ffn, lw.eps), lw.w_gate, lw.w_up), lw.w_down)
+            out[step].append(O.linear(O.rms_norm(h, gain, eps), w_out)[0])
+    return np.array(out)
+
+
+@pytest.mark.parametrize("dtype,window", [("f32", None), ("bf16", None), ("bf16", 2)])
+def test_answer_loop_matches_the_oracle(dtype, window):
+    """Prefill, then 21 tokens of three requests (pages fill and new ones begin): logits in front of every token against the oracle that is fed the
+    same tokens, tokens against the oracle's draw from the library's logits.  Tolerance: a layer's bar of relative error (each of its operators is inside
+    it) per layer and one more for the logits, as a free-running loop inherits them."""
+    steps = 21
+    w, weights, loop, ans, before, model = _answer_setup(dtype, n_layers=2 if window is None else 3, window=window, temperature=[0.8, 0.0, 1.2], top_k=[0, 0, 40], top_p=[0.9, 1.0, 0.95], min_p=0.01)
+    u = np.random.default_rng(3).random((steps, 3), dtype=np.float32)
+    tokens, logprobs, logits = ans.run(u, keep=True)
+    want = _oracle_answer(w, weights, ans, before, model, tokens)
+    bar = (1e-2 if dtype == "bf16" else 2e-5) * (len(weights) + 1)
+    for step in range(steps):
+        for r in range(3):
+            off = np.linalg.norm(logits[step][r] - want[step][r]) / np.linalg.norm(want[step][r])
+            assert off <= bar, f"step {step} request {r}: logits {off:.3e} off"
+            t = (0.8, 0.0, 1.2)[r], (0, 0, 40)[r], float(np.float32((0.9, 1.0, 0.95)[r])), float(np.float32(0.01))
+            drawn = A.sample(logits[step][r], float(np.float32(t[0])), *t[1:], float(u[step, r]))
+            assert tokens[step, r] == drawn[0] and abs(logprobs[step, r] - drawn[1]) <= 2.0 ** -24 * abs(drawn[1]) + 2.0 ** -40
+    assert len(set(tokens[:, 0])) > 3
+    seg = ans.segs.cpu().numpy()
+    assert (seg[np.asarray(w.req_seg_off[1:]) - 1, 3] == [21 + 20, 16 + 20, 3 + 20]).all()
+    with pytest.raises(ValueError):
+        ans.run(u[:1])
+    loop.close()
+
+
+def test_answer_loop_in_a_graph_and_in_pieces():
+    """Steps replayed from a graph, and a run in two pieces: the same bits as eager steps."""
+    u = np.random.default_rng(4).random((18, 3), dtype=np.float32)
+    runs = []
+    for how in ("eager", "graph", "pieces"):
+        _, _, loop, ans, _, _ = _answer_setup("bf16", temperature=1.0, top_p=0.95)
+        if how == "pieces":
+            parts = [ans.run(u[:5], keep=True), ans.run(u[5:], keep=True, graph=True)]
+            runs.append([np.concatenate([a, b]) for a, b in zip(*(p[:2] for p in parts))] + [parts[0][2] + parts[1][2]])
+        else:
+            runs.append(ans.run(u, graph=how == "graph", keep=True))
+        loop.close()
+    for other in runs[1:]:
+        assert np.array_equal(runs[0][0], other[0]) and np.array_equal(runs[0][1], other[1])
+        assert all(np.array_equal(a, b) for a, b in zip(runs[0][2], other[2]))
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_answer_loop_stops(graph):
+    """A request that draws the stop token gets -1 from then on, the others go on as if it were not there."""
+    u = np.random.default_rng(5).random((16, 3), dtype=np.float32)
+    _, _, loop, ans, _, _ = _answer_setup("f32", temperature=1.0)
+    free, _ = ans.run(u)
+    loop.close()
+    stop = int(free[6, 1])
+    _, _, loop, ans, _, _ = _answer_setup("f32", temperature=1.0, stop=stop)
+    got, _ = ans.run(u, graph=graph)
+    for r in range(3):
+        ends = np.nonzero(free[:, r] == stop)[0]
+        n = int(ends[0]) + 1 if len(ends) else len(free)
+        assert np.array_equal(got[:n, r], free[:n, r]) and (got[n:, r] == -1).all()
+    assert (got[7:, 1] == -1).all()
+    loop.close()
