@@ -443,7 +443,8 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
 constexpr int kTileKeys = 64, kTilePages = kTileKeys / kBlock;
 
-template <int D, int CW>
+// (SHARED: values may lie in a second pool)
+template <int D, int CW, bool SHARED>
 __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFreq inv_freq) {
   constexpr int KS = 4 / CW, kStage = D / 32, kImage = 16 * D;          // pieces a thread stages of K (and of V); pieces of an image
   constexpr int kBlocks = 2 / KS;                                      // 32-key blocks of a tile that are this wavefront's
@@ -488,45 +489,57 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   const bf16_t *k_pool = static_cast<const bf16_t*>(a.k_pool) + head_off, *v_pool = static_cast<const bf16_t*>(a.v_pool) + head_off;
   const bf16_t* v_shared = static_cast<const bf16_t*>(a.vs.v_shared) + head_off;
   u32x4 kr[kStage], vr[kStage];
-  int listed = 0;                                                     // pages of the window that count
   // A thread stages the same piece of every 256 / (2 D)-th page, so that page numbers are a wavefront's and addresses a sum with a constant.
   constexpr int kApart = 128 / D;                                     // pages between a thread's
   const int pg0 = wave * 64 / (2 * D), piece = tid % (2 * D), token = piece / (D / 8), half = piece & 1;
   char* const put_k = reinterpret_cast<char*>(image) + ((pg0 * kBlock + token) * (D / 8) + (piece % (D / 8) ^ ((token & 3) | ((token >> 1) & 4)))) * 16;
   char* const put_v = reinterpret_cast<char*>(image) + (8 * D + pg0 * 2 * D + half * D + ((piece >> 1) ^ (4 * half))) * 16;
-  // the tile that begins at entry i of the list, `here` entries of which are this range's
-  auto load = [&](int i, int here) __attribute__((always_inline)) {
+  // What the loop needs of the window's tiles, lane t of tile t: where its pages are, and
+  //   flag 1: slots of it hold no key of this range,  flag 2: some column of the workgroup does not see all of it
+  int w_blk[kTilePages], w_value[SHARED ? kTilePages : 1], w_flags;
+  auto note_window = [&](int here) __attribute__((always_inline)) {
+    w_flags = 0;
 #pragma unroll
-    for (int j = 0; j < kStage; ++j) {
-      const int at = i + pg0 + j * kApart;
-      const Page p = list[min(at, kWindow - 1)];
-      const int blk = __builtin_amdgcn_readfirstlane(p.blk), value = __builtin_amdgcn_readfirstlane(p.value);
-      const int n_valid = at >= here ? 0 : __builtin_amdgcn_readfirstlane(p.n_valid);
-      kr[j] = *reinterpret_cast<const u32x4*>(k_pool + blk * block_elems + piece * 8);
-      const bf16_t* from = value >= 0 ? v_pool + value * block_elems : v_shared + (-1 - value) * block_elems;
-      vr[j] = *reinterpret_cast<const u32x4*>(from + piece * 8);
-      if (n_valid < kBlock) {                                         // padding slots: zeros, or 0 x what lies there would be a product
-        const int left = n_valid - 8 * half;                          // of this thread's eight tokens
-        auto keep = [&](int t) { return (t < left ? 0xffffu : 0u) | (t + 1 < left ? 0xffff0000u : 0u); };
-        vr[j] &= u32x4{keep(0), keep(2), keep(4), keep(6)};
-      }
+    for (int j = 0; j < kTilePages; ++j) {
+      const int at = kTilePages * lane + j;
+      const Page p = list[at];
+      w_blk[j] = p.blk;
+      if (SHARED) w_value[j] = p.value;
+      w_flags |= at >= here || p.n_valid < kBlock ? 1 : 0;
+      w_flags |= at < here && p.pos0 + kBlock - 1 > p_first ? 2 : 0;
     }
   };
-  // ... into image `buf`.  A tile with values that are not finite and that only some columns see is set aside (odd): 0 x such a value would reach
-  // the others.
-  auto store = [&](int buf, int i) __attribute__((always_inline)) {
+  auto of_page = [&](const int* w, int j, int t) __attribute__((always_inline)) {       // entry of this wavefront's j-th page of tile t
+    return __builtin_amdgcn_readlane(kApart == 1 || pg0 == 0 ? w[kApart * j] : w[kApart * j + kApart - 1], t);
+  };
+  auto load = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kStage; ++j) {
+      const int blk = of_page(w_blk, j, t), value = SHARED ? of_page(w_value, j, t) : blk;
+      kr[j] = *reinterpret_cast<const u32x4*>(k_pool + blk * block_elems + piece * 8);
+      const bf16_t* from = !SHARED || value >= 0 ? v_pool + value * block_elems : v_shared + (-1 - value) * block_elems;
+      vr[j] = *reinterpret_cast<const u32x4*>(from + piece * 8);
+    }
+  };
+  // ... into image `buf`.  Values in slots without a key become zeros (0 x what lies there would be a product).  A tile with values that are not finite
+  // and that only some columns see is set aside (odd): 0 x such a value would reach the others.
+  auto store = [&](int buf, int t, int flags, int here) __attribute__((always_inline)) {
+    if (flags != 0) {
+      bool any = false;
+#pragma unroll
+      for (int j = 0; j < kStage; ++j) {
+        const int at = kTilePages * t + pg0 + j * kApart, left = (at < here ? list[at].n_valid : 0) - 8 * half;     // of this thread's eight tokens
+        auto keep = [&](int e) { return (e < left ? 0xffffu : 0u) | (e + 1 < left ? 0xffff0000u : 0u); };
+        auto bad = [](uint32_t v) { return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u; };
+        vr[j] &= u32x4{keep(0), keep(2), keep(4), keep(6)};
+        any |= bad(vr[j][0]) || bad(vr[j][1]) || bad(vr[j][2]) || bad(vr[j][3]);
+      }
+      if ((flags & 2) && __any(any) && lane == 0) odd[t] = 1;
+    }
 #pragma unroll
     for (int j = 0; j < kStage; ++j) {
       *reinterpret_cast<u32x4*>(put_k + buf * (kImage * 16) + j * kApart * 32 * D) = kr[j];
       *reinterpret_cast<u32x4*>(put_v + buf * (kImage * 16) + j * kApart * 32 * D) = vr[j];
-    }
-    // (a tile's last page is the one that lies furthest)
-    if (__builtin_amdgcn_readfirstlane(list[min(i + kTilePages - 1, kWindow - 1)].pos0) + kBlock - 1 > p_first || i + kTilePages > listed) {
-      auto bad = [](uint32_t v) { return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u; };
-      bool any = false;
-#pragma unroll
-      for (int j = 0; j < kStage; ++j) any |= bad(vr[j][0]) || bad(vr[j][1]) || bad(vr[j][2]) || bad(vr[j][3]);
-      if (__any(any) && lane == 0) odd[i / kTilePages] = 1;
     }
   };
 
@@ -550,20 +563,22 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-  float m = -3.4028235e38f, l = 0.f;
+  float m = 0.f, l = 0.f;
+  bool begun = false;                                                 // the column has seen a key, m is a reference of its own
   // byte of this lane's key operand in an image: row of the block as token of its two pages; piece 2 kk + h is this one's, bits of kk flipped
   const int k_row = (n >> 4) * kBlock + ((n >> 2) & 1) * 8 + ((n >> 3) & 1) * 4 + (n & 3);
   const int k_byte = ((ks * kBlocks * 32 + k_row) * (D / 8) + (h ^ ((k_row & 3) | ((k_row >> 1) & 4)))) * 16, v_byte = (8 * D + ks * kBlocks * 4 * D + h * D + (n ^ (4 * h))) * 16;
 
-  // One tile.  ODD: one that was set aside.  p: the tile's pages, page lane % 4 in each lane.
-  auto compute = [&](auto set_aside, const u32x4* img, const Page& p) __attribute__((always_inline)) {
+  // One tile.  ODD: one that was set aside.  i: its first entry of the list, of which `here` count.
+  auto compute = [&](auto set_aside, const u32x4* img, int i, int here, int flags) __attribute__((always_inline)) {
     constexpr bool ODD = decltype(set_aside)::value;
     const int b0 = ks * kBlocks;                                       // this wavefront's first 32-key block
+    // the logits less the reference of the column, which enters as the products' first summand
     f32x16 s[kBlocks];
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
+      for (int e = 0; e < 16; ++e) s[b][e] = -m;
     // (the operands' addresses are made here again: kept over the loop they would cost a register each)
     const char* bytes = reinterpret_cast<const char*>(img);
     int k_at = k_byte;
@@ -575,13 +590,14 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
         const bf16x8 k = *reinterpret_cast<const bf16x8*>(bytes + (k_at ^ (32 * kk)) + b * 64 * D);
         s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[kk], s[b], 0, 0, 0);
       }
-    if (!__all(p.n_valid == kBlock && p.pos0 + kBlock - 1 <= p_min)) {
+    if (flags != 0) {
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          const int pg = (b0 + b) * 2 + g;
-          const int seen = min(__shfl(p.n_valid, pg, 64) - 8 * h, pos - (__shfl(p.pos0, pg, 64) + 8 * h) + 1);
+          const int at = i + (b0 + b) * 2 + g;
+          const Page p = list[at];
+          const int seen = min((at < here ? p.n_valid : 0) - 8 * h, pos - (p.pos0 + 8 * h) + 1);
 #pragma unroll
           for (int e = 0; e < 8; ++e) s[b][8 * g + e] = e < seen ? s[b][8 * g + e] : -INFINITY;
         }
@@ -591,13 +607,20 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
       for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
-    if (__any(top > m + kSlack)) {
+    if (__any(top > kSlack || (!begun && top > -INFINITY))) {
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float m_new = fmaxf(m, top), f = exp2f(m - m_new);
-      m = m_new;
+      const bool first = !begun && top > -INFINITY;
+      top = first ? top : fmaxf(top, 0.f);                             // how far the reference moves
+      begun |= first;
+      const float f = first ? 0.f : exp2f(-top);
+      m += top;
       l *= f;
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) o[j] *= f;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[b][e] -= top;
     }
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
@@ -606,7 +629,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
         bf16x8 w;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float x = __builtin_amdgcn_exp2f(s[b][8 * g + e] - m);
+          const float x = __builtin_amdgcn_exp2f(s[b][8 * g + e]);
           l += x;
           w[e] = static_cast<bf16_t>(x);
         }
@@ -625,7 +648,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
             for (int e = 0; e < 8; ++e) v[e] = fabsf(to_float(v[e])) < INFINITY ? v[e] : static_cast<bf16_t>(0.f);
             o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, o[j], 0, 0, 0);
           }
-          const int first = __shfl(p.pos0, pg, 64);
+          const int first = list[i + pg].pos0;
           const bf16_t* values = reinterpret_cast<const bf16_t*>(img + 8 * D + pg * 2 * D);
 #pragma unroll 1
           for (int t = 0; t < kBlock; ++t) {
@@ -651,11 +674,6 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   };
 
   // ---- the keys, until no column of the workgroup sees them
-  auto pages_at = [&](int i, int here) __attribute__((always_inline)) {
-    Page p = list[min(i + (lane & 3), kWindow - 1)];
-    if (i + (lane & 3) >= here) p.n_valid = 0;
-    return p;
-  };
   for (int at = first_page; at == first_page || at < end_page; at += kWindow) {
     if (at > first_page) list_pages(a, s_begin, s_end, at, list, scratch.segs, scratch.seg_end, scratch.wave_pages, &end_pos);
     if (tid < kWindow / kTilePages) odd[tid] = 0;
@@ -663,31 +681,38 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     if (a.k_new != nullptr) write_rows<bf16_t, D>(a, inv_freq, list, in_range, split == 0 && at == first_page, s_end > s_begin ? end_pos : 0, row0, n_cols / group, kvh);
     // (pages are in the order of their positions; one that does not exist has no keys)
     const int here = __syncthreads_count(tid < in_range && (list[tid].pos0 <= p_last || list[tid].n_valid == 0)), tiles = (here + kTilePages - 1) / kTilePages;
-    listed = here;
+    note_window(here);
+    auto flags_of = [&](int t) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(w_flags, t); };
     if (tiles > 0) {
-      load(0, here);
-      store(0, 0);
-      if (tiles > 1) load(kTilePages, here);
+      load(0);
+      store(0, 0, flags_of(0), here);
+      if (tiles > 1) load(1);
     }
     __syncthreads();
+    bool aside = false;                                               // (of this window some tile)
     for (int t = 0; t < tiles; ++t) {
-      if (t + 1 < tiles) store((t + 1) & 1, (t + 1) * kTilePages);
-      if (t + 2 < tiles) load((t + 2) * kTilePages, here);
-      if (odd[t] == 0) compute(std::false_type(), image + (t & 1) * kImage, pages_at(t * kTilePages, here));
+      if (t + 1 < tiles) store((t + 1) & 1, t + 1, flags_of(t + 1), here);
+      if (t + 2 < tiles) load(t + 2);
+      const int flags = flags_of(t);
+      const bool skip = (flags & 2) != 0 && __builtin_amdgcn_readfirstlane(odd[t]) != 0;
+      aside |= skip;
+      if (!skip) compute(std::false_type(), image + (t & 1) * kImage, t * kTilePages, here, flags);
       __syncthreads();
     }
-    for (int t = 0; t < tiles; ++t)
-      if (odd[t] != 0) {
-        load(t * kTilePages, here);
-        store(0, t * kTilePages);
-        __syncthreads();
-        compute(std::true_type(), image, pages_at(t * kTilePages, here));
-        __syncthreads();
-      }
+    if (aside)
+      for (int t = 0; t < tiles; ++t)
+        if (odd[t] != 0) {
+          load(t);
+          store(0, t, flags_of(t), here);
+          __syncthreads();
+          compute(std::true_type(), image, t * kTilePages, here, flags_of(t));
+          __syncthreads();
+        }
   }
 
   // ---- results
   l += __shfl_xor(l, 32, 64);
+  m = begun ? m : -3.4028235e38f;
   float* mine = reinterpret_cast<float*>(image);
   if constexpr (KS == 2) {
     // the second stream's sums go through LDS to the first one's lanes: [value][lane]
@@ -879,8 +904,11 @@ static void launch_append_t(const cc_ctx* ctx, const AppendArgs& a, const Append
   const dim3 grid(static_cast<unsigned>(p.groups));
   if (p.cols == 16) hipLaunchKernelGGL((append_split_kernel<T, D>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
   if constexpr (sizeof(T) == 2) {
-    if (p.cols == 64) hipLaunchKernelGGL((append_tile_kernel<D, 2>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
-    if (p.cols == 128) hipLaunchKernelGGL((append_tile_kernel<D, 4>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
+    const bool shared = a.vs.v_map != nullptr;
+    if (p.cols == 64 && !shared) hipLaunchKernelGGL((append_tile_kernel<D, 2, false>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
+    if (p.cols == 64 && shared) hipLaunchKernelGGL((append_tile_kernel<D, 2, true>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
+    if (p.cols == 128 && !shared) hipLaunchKernelGGL((append_tile_kernel<D, 4, false>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
+    if (p.cols == 128 && shared) hipLaunchKernelGGL((append_tile_kernel<D, 4, true>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
   }
   const int n_items = n_q_tot * a.hq;
   if (p.n_splits > 8) hipLaunchKernelGGL((append_join_kernel<T, D, true>), dim3(n_items), dim3(256), 0, stream, a, n_items);
