@@ -570,29 +570,58 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   const int k_byte = ((ks * kBlocks * 32 + k_row) * (D / 8) + (h ^ ((k_row & 3) | ((k_row >> 1) & 4)))) * 16, v_byte = (8 * D + ks * kBlocks * 4 * D + h * D + (n ^ (4 * h))) * 16;
 
   // One tile.  ODD: one that was set aside.  i: its first entry of the list, of which `here` count.
+  // In the order  S(0), S(1) with the exponentials of block 0 under its products, P V(0) with those of block 1, P V(1), four operands read ahead; the
+  // steps are fenced, because the compiler by itself reads every operand right in front of its product and takes the exponentials together.
   auto compute = [&](auto set_aside, const u32x4* img, int i, int here, int flags) __attribute__((always_inline)) {
     constexpr bool ODD = decltype(set_aside)::value;
+    constexpr int kSteps = D / 16, kAhead = kSteps < 4 ? kSteps : 4;   // products of a block; operands in flight
     const int b0 = ks * kBlocks;                                       // this wavefront's first 32-key block
-    // the logits less the reference of the column, which enters as the products' first summand
-    f32x16 s[kBlocks];
-#pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[b][e] = -m;
     // (the operands' addresses are made here again: kept over the loop they would cost a register each)
     const char* bytes = reinterpret_cast<const char*>(img);
     int k_at = k_byte;
     asm volatile("" : "+v"(k_at));
+    auto key = [&](int b, int kk) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8*>(bytes + (k_at ^ (32 * kk)) + b * 64 * D); };
+    auto value = [&](int b, int g, int j) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8*>(bytes + v_byte + (2 * b + g) * 32 * D + j * 512); };
+    f32x16 s[kBlocks];
+    bf16x8 w[kBlocks][2];
+    // the logits less the reference of the column, which enters as the products' first summand
+    auto fence = []() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
+    // weights of the two logits 2 x, 2 x + 1 of a block
+    auto weigh = [&](int b, int x) __attribute__((always_inline)) {
+      const float x0 = __builtin_amdgcn_exp2f(s[b][2 * x]), x1 = __builtin_amdgcn_exp2f(s[b][2 * x + 1]);
+      l += x0;
+      l += x1;
+      w[b][x / 4][2 * x % 8] = static_cast<bf16_t>(x0);
+      w[b][x / 4][2 * x % 8 + 1] = static_cast<bf16_t>(x1);
+    };
+    // S(b); under it the weights of block `under` (-1: none)
+    auto products = [&](int b, auto under) __attribute__((always_inline)) {
+      bf16x8 k[kAhead];
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk)
+      for (int kk = 0; kk < kAhead; ++kk) k[kk] = key(b, kk);
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-        const bf16x8 k = *reinterpret_cast<const bf16x8*>(bytes + (k_at ^ (32 * kk)) + b * 64 * D);
-        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[kk], s[b], 0, 0, 0);
+      for (int e = 0; e < 16; ++e) s[b][e] = -m;
+      fence();
+#pragma unroll
+      for (int kk = 0; kk < kSteps; ++kk) {
+        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kk % kAhead], q[kk], s[b], 0, 0, 0);
+        if (kk + kAhead < kSteps) k[kk % kAhead] = key(b, kk + kAhead);
+        if constexpr (decltype(under)::value >= 0)
+#pragma unroll
+          for (int x = 0; x < 8 / kSteps; ++x) weigh(decltype(under)::value, kk * (8 / kSteps) + x);
+        fence();
       }
-    if (flags != 0) {
+      if constexpr (decltype(under)::value >= 0)
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
+        for (int g = 0; g < 2; ++g) {                                  // (the weights are made here, not behind the next branch)
+          u32x4 bits = __builtin_bit_cast(u32x4, w[decltype(under)::value][g]);
+          asm volatile("" : "+v"(bits));
+          w[decltype(under)::value][g] = __builtin_bit_cast(bf16x8, bits);
+        }
+    };
+    // masks, and the reference where a logit lies too far above it; done: blocks whose weights are made but not multiplied yet
+    auto settle = [&](int b, int done) __attribute__((always_inline)) {
+      if (flags != 0) {
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           const int at = i + (b0 + b) * 2 + g;
@@ -601,54 +630,60 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
 #pragma unroll
           for (int e = 0; e < 8; ++e) s[b][8 * g + e] = e < seen ? s[b][8 * g + e] : -INFINITY;
         }
-    }
-    float top = s[0][0];
+      }
+      float top = s[b][0];
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
+      for (int e = 1; e < 16; ++e) top = fmaxf(top, s[b][e]);
+      if (__any(top > kSlack || (!begun && top > -INFINITY))) {
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const bool first = !begun && top > -INFINITY;
+        top = first ? top : fmaxf(top, 0.f);                           // how far the reference moves
+        begun |= first;
+        const float f = first ? 0.f : exp2f(-top);
+        m += top;
+        l *= f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
-    if (__any(top > kSlack || (!begun && top > -INFINITY))) {
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const bool first = !begun && top > -INFINITY;
-      top = first ? top : fmaxf(top, 0.f);                             // how far the reference moves
-      begun |= first;
-      const float f = first ? 0.f : exp2f(-top);
-      m += top;
-      l *= f;
-#pragma unroll
-      for (int j = 0; j < D / 32; ++j) o[j] *= f;
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
+        for (int j = 0; j < D / 32; ++j) o[j] *= f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[b][e] -= top;
-    }
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
+        for (int d = 0; d < done; ++d)
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        bf16x8 w;
+          for (int g = 0; g < 2; ++g)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float x = __builtin_amdgcn_exp2f(s[b][8 * g + e]);
-          l += x;
-          w[e] = static_cast<bf16_t>(x);
+            for (int e = 0; e < 8; ++e) w[d][g][e] = static_cast<bf16_t>(to_float(w[d][g][e]) * f);
+      }
+    };
+    // o += V P(b); under it the weights of block `under`
+    auto add_values = [&](int b, auto under) __attribute__((always_inline)) {
+      if constexpr (!ODD) {
+        bf16x8 v[4];
+        constexpr int kV = D / 16;                                     // products: two pages of D / 32 groups of dims
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[x] = value(b, x / (D / 32), x % (D / 32));
+        fence();
+#pragma unroll
+        for (int x = 0; x < kV; ++x) {
+          const int j = x % (D / 32);
+          o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[x % 4], w[b][x / (D / 32)], o[j], 0, 0, 0);
+          if (x + 4 < kV) v[x % 4] = value(b, (x + 4) / (D / 32), (x + 4) % (D / 32));
+          if constexpr (decltype(under)::value >= 0)
+#pragma unroll
+            for (int y = 0; y < 8 / kV; ++y) weigh(decltype(under)::value, x * (8 / kV) + y);
+          fence();
         }
-        const int pg = (b0 + b) * 2 + g;
-        const char* v_at = bytes + v_byte + (2 * b + g) * 32 * D;
-        if constexpr (!ODD) {
+      } else {
+        // the values that are not finite leave the product and are added to the columns that see them
 #pragma unroll
-          for (int j = 0; j < D / 32; ++j)
-            o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(v_at + j * 512), w, o[j], 0, 0, 0);
-        } else {
-          // the values that are not finite leave the product and are added to the columns that see them
+        for (int g = 0; g < 2; ++g) {
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) {
-            bf16x8 v = *reinterpret_cast<const bf16x8*>(v_at + j * 512);
+            bf16x8 v = value(b, g, j);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = fabsf(to_float(v[e])) < INFINITY ? v[e] : static_cast<bf16_t>(0.f);
-            o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, o[j], 0, 0, 0);
+            o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[b][g], o[j], 0, 0, 0);
           }
-          const int first = list[i + pg].pos0;
+          const int pg = (b0 + b) * 2 + g, first = list[i + pg].pos0;
           const bf16_t* values = reinterpret_cast<const bf16_t*>(img + 8 * D + pg * 2 * D);
 #pragma unroll 1
           for (int t = 0; t < kBlock; ++t) {
@@ -656,7 +691,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
             asm volatile("" : "+v"(dim0));
             float weight = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) weight = t % 8 == e ? to_float(w[e]) : weight;
+            for (int e = 0; e < 8; ++e) weight = t % 8 == e ? to_float(w[b][g][e]) : weight;
             weight = __shfl(weight, n + 32 * (t >> 3), 64);
             const bool sees = first + t <= pos;
 #pragma unroll
@@ -671,6 +706,29 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
           }
         }
       }
+    };
+    constexpr std::integral_constant<int, -1> none;
+    constexpr std::integral_constant<int, 0> first_block;
+    constexpr std::integral_constant<int, 1> second_block;
+    products(0, none);
+    settle(0, 0);
+    if constexpr (kBlocks == 2 && !ODD) {
+      products(1, first_block);
+      settle(1, 1);
+      add_values(0, second_block);
+      add_values(1, none);
+    } else {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) weigh(0, x);
+      add_values(0, none);
+      if constexpr (kBlocks == 2) {
+        products(1, none);
+        settle(1, 0);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) weigh(1, x);
+        add_values(1, none);
+      }
+    }
   };
 
   // ---- the keys, until no column of the workgroup sees them
