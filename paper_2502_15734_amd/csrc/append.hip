@@ -710,6 +710,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     constexpr std::integral_constant<int, -1> none;
     constexpr std::integral_constant<int, 0> first_block;
     constexpr std::integral_constant<int, 1> second_block;
+    __builtin_amdgcn_s_setprio(1);                                     // (2 %: a wavefront that stages or waits stands back)
     products(0, none);
     settle(0, 0);
     if constexpr (kBlocks == 2 && !ODD) {
@@ -729,6 +730,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
         add_values(1, none);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
   };
 
   // ---- the keys, until no column of the workgroup sees them
