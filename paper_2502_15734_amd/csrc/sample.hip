@@ -254,29 +254,32 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const R
   }
 }
 
-// The weights of a row in parts: 2^(y / 64) with y = (z - max z) 64 / (T ln 2), as a table of 2^(j / 64) and the series of 2^(f / 64), |f| <= 1/2, to f^5
-// (the rest is below 2^-54), times 2^shift.
-constexpr int kTable = 64;
+// The weights of a row in parts: 2^(y / 256) with y = (z - max z) 256 / (T ln 2), as a table of 2^(j / 256) and the series of 2^(f / 256), |f| <= 1/2,
+// to f^4 (the rest is below 2^-54), times 2^shift.  The passes over a large vocabulary are bound by these steps in 64 bits, so the
+// nearest whole number is the last bits of a sum and the exponent is added to the table's entry as an integer.
+constexpr int kTable = 256;
 struct Weights {
   double top, per, least;             // least: min_p in the same units
   const double* table;
   int shift;
-  // table: [kTable] in LDS, filled here by the first threads (a barrier has to follow)
+  // table: [kTable] in LDS, filled here by the workgroup (a barrier has to follow)
   __device__ __forceinline__ Weights(float top_logit, const RowSettings& s, int shift_, double* table_)
-      : top(top_logit), per(s.inv_t * 92.33248261689366), least(ldexp(s.min_p, shift_)), table(table_), shift(shift_) {       // 64 / ln 2
-    if (threadIdx.x < kTable) table_[threadIdx.x] = exp_of(threadIdx.x * 0.010830424696249145);       // ln 2 / 64
+      : top(top_logit), per(s.inv_t * 369.3299304675746), least(ldexp(s.min_p, shift_)), table(table_), shift(shift_) {       // 256 / ln 2
+    static_assert(kTable <= 256, "one entry a thread");
+    if (threadIdx.x < kTable) table_[threadIdx.x] = exp_of(threadIdx.x * 0.0027076061740622863);       // ln 2 / 256
   }
   // w 2^shift; exactly 2^shift for the largest logit
   __device__ __forceinline__ double scaled(float z) const {
-    const double y = fmax((static_cast<double>(z) - top) * per, -64.0 * 900.0), n = rint(y), f = y - n;
-    double p = 1.2417843701716925e-12;                                     // (ln 2 / 64)^5 / 5! and so on down
-    p = fma(p, f, 5.732851688640402e-10);
-    p = fma(p, f, 2.1173137155464776e-07);
-    p = fma(p, f, 5.86490495505617e-05);
-    p = fma(p, f, 0.010830424696249145);
+    const double y = fmax((static_cast<double>(z) - top) * per, -256.0 * 900.0), t = y + 0x1.8p52, f = y - (t - 0x1.8p52);       // (t: its low word is the nearest whole number)
+    const int n = static_cast<int>(__double_as_longlong(t));
+    double p = 2.239395190875157e-12;                                      // (ln 2 / 256)^4 / 4! and so on down
+    p = fma(p, f, 3.3083026805413713e-09);
+    p = fma(p, f, 3.6655655969101062e-06);
+    p = fma(p, f, 0.0027076061740622863);
     p = fma(p, f, 1.0);
-    const int i = static_cast<int>(n);
-    return ldexp(table[i & (kTable - 1)] * p, (i >> 6) + shift);
+    // (2^-900 2^shift and more: the exponent stays that of a normal number)
+    const double e = table[n & (kTable - 1)];
+    return __hiloint2double(__double2hiint(e) + (((n >> 8) + shift) << 20), __double2loint(e)) * p;
   }
   // ... to the nearest whole number (shift <= 50: the sum with 2^52 has it in its last bits)
   static __device__ __forceinline__ unsigned long long whole(double w) {
@@ -618,6 +621,57 @@ __device__ __forceinline__ unsigned long long block_before(unsigned long long v,
   return in - v;
 }
 
+// n_pow (a power of two, E N or at most N) places of LDS by N threads, the largest in front: bitonic, with place e N + t in thread t's register e.
+// Exchanges over less than 64 places go through the wavefront's lanes, over N and more between a thread's registers, and only those
+// between through LDS: of a list of 512 by 256 threads 5 steps of 45.
+template <int E, int N>
+__device__ __forceinline__ void sort_down(unsigned long long* order, int n_pow) {
+  const int tid = threadIdx.x;
+  const bool on = E > 1 || tid < n_pow;
+  unsigned long long v[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = on ? order[e * N + tid] : 0ull;
+  // (place, distance, length: whether the place takes the larger one)
+  auto larger = [](int at, int half, int len) { return ((at & half) == 0) == ((at & len) == 0); };
+  for (int len = 2; len <= n_pow; len <<= 1)
+    for (int half = len >> 1; half > 0; half >>= 1) {
+      if (half >= N) {
+#pragma unroll
+        for (int step = 1; step < E; step <<= 1)
+          if (half == step * N)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+              if ((e & step) == 0) {
+                const unsigned long long a = v[e], b = v[e | step];
+                const bool up = larger(e * N + tid, half, len) == (a > b);
+                v[e] = up ? a : b;
+                v[e | step] = up ? b : a;
+              }
+        continue;
+      }
+      unsigned long long u[E];
+      if (half < 64) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) u[e] = __shfl_xor(v[e], half, 64);
+      } else {
+        __syncthreads();
+        if (on)
+#pragma unroll
+          for (int e = 0; e < E; ++e) order[e * N + tid] = v[e];
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < E; ++e) u[e] = on ? order[(e * N + tid) ^ half] : 0ull;
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = larger(e * N + tid, half, len) == (v[e] > u[e]) ? v[e] : u[e];
+    }
+  __syncthreads();
+  if (on)
+#pragma unroll
+    for (int e = 0; e < E; ++e) order[e * N + tid] = v[e];
+  __syncthreads();
+}
+
 // W wavefronts.
 template <typename T, int W>
 __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, SamplePlan plan, RowScratch* __restrict__ scratch) {
@@ -701,42 +755,18 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
     sample_row<T, W>(a, row, s, top, sh.row);
     return;
   }
-  // ---- the candidates in order: largest logit, then lowest index.  Bitonic; a list that gives a thread one candidate exchanges in a
-  // wavefront's own lanes as far as these reach, otherwise through LDS.
+  // ---- the candidates in order
   int n_pow = 1;
   while (n_pow < n_list) n_pow <<= 1;
   for (int i = n_list + tid; i < n_pow; i += kThreads) sh.list.order[i] = 0ull;
   for (int i = tid; i < n_tiles; i += kThreads) sh.list.tile[i] = parts ? scratch[row].tile_mass[i] : 0ull;
   __syncthreads();
-  if (n_pow <= kThreads) {
-    unsigned long long v = tid < n_pow ? sh.list.order[tid] : 0ull;
-    for (int len = 2; len <= n_pow; len <<= 1)
-      for (int half = len >> 1; half > 0; half >>= 1) {
-        unsigned long long u;
-        if (half < 64) {
-          u = __shfl_xor(v, half, 64);
-        } else {
-          __syncthreads();
-          if (tid < n_pow) sh.list.order[tid] = v;
-          __syncthreads();
-          u = tid < n_pow ? sh.list.order[tid ^ half] : 0ull;
-        }
-        const bool larger = ((tid & half) == 0) == ((tid & len) == 0);            // this place takes the larger one
-        v = larger ? (v > u ? v : u) : (v < u ? v : u);
-      }
-    __syncthreads();
-    if (tid < n_pow) sh.list.order[tid] = v;
-    __syncthreads();
-  } else {
-    for (int len = 2; len <= n_pow; len <<= 1)
-      for (int half = len >> 1; half > 0; half >>= 1) {
-        for (int i = tid; i < n_pow / 2; i += kThreads) {
-          const int lo = (i / half) * 2 * half + i % half, hi = lo + half;
-          const unsigned long long u = sh.list.order[lo], v = sh.list.order[hi];
-          if ((u < v) == ((lo & len) == 0)) { sh.list.order[lo] = v; sh.list.order[hi] = u; }
-        }
-        __syncthreads();
-      }
+  if (n_pow <= kThreads) sort_down<1, kThreads>(sh.list.order, n_pow);
+  else if (n_pow == 2 * kThreads) sort_down<2, kThreads>(sh.list.order, n_pow);
+  else if (n_pow == 4 * kThreads) sort_down<4, kThreads>(sh.list.order, n_pow);
+  else if constexpr (kList > 4 * kThreads) {
+    if (n_pow == 8 * kThreads) sort_down<8, kThreads>(sh.list.order, n_pow);
+    else sort_down<16, kThreads>(sh.list.order, n_pow);
   }
   // ---- the cut among them.  This thread's are own .. own + per
   const int per = max(1, n_pow / kThreads), own = tid * per;
