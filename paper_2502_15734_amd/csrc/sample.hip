@@ -299,6 +299,14 @@ struct Part {
   float top, low;                     // largest and smallest logit (top -inf: none)
   int top_idx, unused;
 };
+struct Cuts {
+  int p_lo, p_hi, k_bin;              // candidates: bins p_lo .. p_hi, and k_bin; bins in front of p_lo are kept whole
+  unsigned count_lo, count_hi;        // tokens in front of p_lo, behind p_hi
+  unsigned count_k;                   // tokens in front of k_bin
+  unsigned listed;                    // candidates
+  unsigned long long mass_lo, mass_k, mass_all;      // weights in front of p_lo, of k_bin, of all bins
+};
+
 struct RowScratch {
   Part part[kMaxParts];
   unsigned long long mass[kBins];
@@ -307,6 +315,7 @@ struct RowScratch {
   unsigned count[kBins];
   unsigned tile_kept[kTiles];
   unsigned n_list, unused[3];
+  Cuts cuts;                          // (of a row that needs a cut and has bins)
 };
 
 // The row as pieces of 16 bytes at aligned addresses: element e of them is logit e - shift.
@@ -322,9 +331,9 @@ struct RowReader {
   }
   typedef __attribute__((__vector_size__(16))) T Piece;
   // f(logit, index) for the row's elements e0 .. e0 + kPer, e0 + step .., up to e1 (multiples of kPer), in the order of the indexes; kAhead pieces are
-  // loaded before the first is used.  Only the row's own logits are read; -inf and NaN are passed over.
+  // loaded before the first is used.  Only the row's own logits are read; -inf and NaN are passed over, and pieces with nothing from `least` up.
   template <typename F>
-  __device__ __forceinline__ void each(int e0, int e1, int step, F&& f) const {
+  __device__ __forceinline__ void each(int e0, int e1, int step, float least, F&& f) const {
     constexpr int kAhead = 4;
     for (int e = e0; e < e1; e += kAhead * step) {
       Piece v[kAhead];
@@ -338,6 +347,12 @@ struct RowReader {
         const int i = e + a * step - shift;
         if (e + a * step >= e1) break;
         const bool whole = i >= 0 && i + kPer <= vocab;
+        if (whole) {
+          float most = to_float(v[a][0]);
+#pragma unroll
+          for (int j = 1; j < kPer; ++j) most = fmaxf(most, to_float(v[a][j]));
+          if (most < least) continue;
+        }
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
           if (!whole && (i + j < 0 || i + j >= vocab)) continue;
@@ -378,18 +393,10 @@ struct Bins {
   __device__ __forceinline__ int of(float z) const { return static_cast<int>(fminf((top - z) * per, static_cast<float>(kBins - 1))); }
 };
 
-struct Cuts {
-  int p_lo, p_hi, k_bin;              // candidates: bins p_lo .. p_hi, and k_bin; bins in front of p_lo are kept whole
-  unsigned count_lo, count_hi;        // tokens in front of p_lo, behind p_hi
-  unsigned count_k;                   // tokens in front of k_bin
-  unsigned listed;                    // candidates
-  unsigned long long mass_lo, mass_k, mass_all;      // weights in front of p_lo, of k_bin, of all bins
-};
-
 // Where the cuts fall, from the histogram.  With both top-k and top-p the weight that top-p refers to is known to the bin that top-k's cut
 // falls into, so top-p's has a first and a last possible bin.
 template <int N>
-__device__ __forceinline__ Cuts find_cuts(const RowScratch& ws, const RowSettings& s, int vocab) {
+__device__ __forceinline__ Cuts find_cuts(const RowScratch& ws, const RowSettings& s) {
   constexpr int kOwn = kBins / N;     // bins of a thread
   __shared__ unsigned long long wave_mass[N / 64];
   __shared__ unsigned wave_count[N / 64];
@@ -475,7 +482,7 @@ __global__ __launch_bounds__(256) void sample_max_kernel(SampleArgs a, SamplePla
   float top = -INFINITY, low = INFINITY;
   int at = 0x7fffffff;
   const int e1 = min((part + 1) * plan.part_len, a.vocab + in.shift);
-  in.each(part * plan.part_len + tid * kPer, e1, 256 * kPer, [&](float z, int i) __attribute__((always_inline)) {
+  in.each(part * plan.part_len + tid * kPer, e1, 256 * kPer, -INFINITY, [&](float z, int i) __attribute__((always_inline)) {
     if (z > top) { top = z; at = i; }
     low = fminf(low, z);
   });
@@ -518,7 +525,7 @@ __global__ __launch_bounds__(256) void sample_hist_kernel(SampleArgs a, SamplePl
   const RowReader<T> in(a, row);
   const bool weigh = s.top_p < 1.0;
   const int e1 = min((part + 1) * plan.part_len, a.vocab + in.shift);
-  in.each(part * plan.part_len + tid * kPer, e1, 256 * kPer, [&](float z, int) __attribute__((always_inline)) {
+  in.each(part * plan.part_len + tid * kPer, e1, 256 * kPer, -INFINITY, [&](float z, int) __attribute__((always_inline)) {
     const int b = bins.of(z);
     atomicAdd(&count[b], 1u);
     if (weigh) atomicAdd(&mass[b], Weights::whole(weights.scaled(z)));
@@ -550,21 +557,28 @@ __global__ __launch_bounds__(256) void sample_tiles_kernel(SampleArgs a, SampleP
   __syncthreads();
   int p_lo = kBins, p_hi = kBins, k_bin = kBins;
   if (cut) {
-    const Cuts c = find_cuts<256>(ws, s, a.vocab);
+    const Cuts c = find_cuts<256>(ws, s);
+    if (part == 0 && tid == 0) ws.cuts = c;
     if (c.listed > kList) return;                      // (the last kernel does the row alone)
     p_lo = c.p_lo; p_hi = c.p_hi; k_bin = c.k_bin;
   }
   const RowReader<T> in(a, row);
   const int tile0 = (part * 4 + wave) * plan.wave_tiles;
+  // (logits below least_z are below min-p for certain, and those below floor are neither kept nor candidates: 2^-20 and a bin for the roundings)
+  const double reach = log(s.min_p) / s.inv_t;         // (-inf without min-p; a NaN: no such logit)
+  const float least_z = static_cast<float>(weights.top + reach - 0x1p-20 * (fabs(weights.top) - reach));
+  const int last_bin = k_bin < kBins ? max(p_hi, k_bin) : p_hi;
+  const float floor = !cut ? least_z : last_bin < kBins - 2 ? x.top - (last_bin + 2) / bins.per : -INFINITY;
   unsigned kept[4] = {0, 0, 0, 0};
   unsigned long long sum[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int t = 0; t < 4; ++t)
     if (t < plan.wave_tiles) {
       const int e0 = (tile0 + t) * plan.tile_len;
-      in.each(e0 + lane * kPer, min(e0 + plan.tile_len, a.vocab + in.shift), 64 * kPer, [&](float z, int i) __attribute__((always_inline)) {
+      in.each(e0 + lane * kPer, min(e0 + plan.tile_len, a.vocab + in.shift), 64 * kPer, floor, [&](float z, int i) __attribute__((always_inline)) {
         const int b = cut ? bins.of(z) : -1;
         if (b < p_lo) {
+          if (z < least_z) return;
           const double w = weights.scaled(z);
           if (w >= weights.least) { ++kept[t]; sum[t] += Weights::whole(w); }
         } else if (b <= p_hi || b == k_bin) {
@@ -696,8 +710,16 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
   Cuts c{0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
   int n_list = 0;
   bool whole = false;                                  // the list does not hold the candidates
+  // (what the other kernels left, in one trip to memory; what this row does not use is not looked at)
+  uint2 listed{0, 0};
+  unsigned long long tile_mass = 0;
+  unsigned tile_kept = 0;
   if (parts) {
-    x = row_extremes(scratch[row], plan.parts);
+    const RowScratch& ws = scratch[row];
+    c = ws.cuts;
+    listed = ws.list[tid];
+    if (tid < n_tiles) { tile_mass = ws.tile_mass[tid]; tile_kept = ws.tile_kept[tid]; }
+    x = row_extremes(ws, plan.parts);
     top = logit_key(x.top);
     top_idx = x.top_idx;
   } else {
@@ -742,12 +764,11 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
   const Weights weights(top_logit, s, a.shift, table);
   __syncthreads();
   if (!whole && parts && cut) {
-    c = find_cuts<kThreads>(scratch[row], s, a.vocab);
     whole = c.listed > kList;
     n_list = static_cast<int>(c.listed);
     if (!whole)
       for (int i = tid; i < n_list; i += kThreads) {
-        const uint2 v = scratch[row].list[i];
+        const uint2 v = i == tid ? listed : scratch[row].list[i];
         sh.list.order[i] = (static_cast<unsigned long long>(v.x) << 32) | ~v.y;
       }
   }
@@ -759,7 +780,7 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
   int n_pow = 1;
   while (n_pow < n_list) n_pow <<= 1;
   for (int i = n_list + tid; i < n_pow; i += kThreads) sh.list.order[i] = 0ull;
-  for (int i = tid; i < n_tiles; i += kThreads) sh.list.tile[i] = parts ? scratch[row].tile_mass[i] : 0ull;
+  if (tid < n_tiles) sh.list.tile[tid] = tile_mass;   // (n_tiles is at most the number of threads)
   __syncthreads();
   if (n_pow <= kThreads) sort_down<1, kThreads>(sh.list.order, n_pow);
   else if (n_pow == 2 * kThreads) sort_down<2, kThreads>(sh.list.order, n_pow);
@@ -808,9 +829,9 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
   const unsigned long long last = kept_list > 0 ? sh.list.order[kept_list - 1] : ~0ull;     // (key, ~index) of the last kept candidate
   __syncthreads();
   // ---- the tile the number falls into
-  const unsigned long long here = tid < n_tiles ? sh.list.tile[tid] : 0ull;               // (n_tiles is at most the number of threads)
+  const unsigned long long here = tid < n_tiles ? sh.list.tile[tid] : 0ull;
   const unsigned long long front = block_before<W>(here, part_mass), total = block_sum<W>(here, part_mass);
-  const unsigned n_kept = block_sum<W>(parts && tid < n_tiles ? scratch[row].tile_kept[tid] : 0u, part_count) + kept_list;
+  const unsigned n_kept = block_sum<W>(tile_kept, part_count) + kept_list;
   const double target = s.u * static_cast<double>(total);
   if (static_cast<double>(front) <= target && static_cast<double>(front + here) > target) { found = tid; found_before = front; }
   __syncthreads();
@@ -845,7 +866,8 @@ SamplePlan sample_plan(int n_rows, int vocab) {
   SamplePlan p{0, 0, 0, 0};
   if (vocab <= kList) return p;
   const long long wanted = std::max(1, std::min(kMaxParts, 1024 / std::max(1, n_rows)));
-  const long long len = std::max((vocab + 8 + wanted - 1) / wanted, 2048ll);      // (8: a row's beginning inside a piece)
+  const long long most = (vocab + 8 + kMaxParts - 1) / kMaxParts;                  // (8: a row's beginning inside a piece)
+  const long long len = std::max(most, std::min<long long>(std::max((vocab + 8 + wanted - 1) / wanted, 2048ll), 8192));
   p.part_len = static_cast<int>((len + 2047) / 2048 * 2048);
   p.parts = (vocab + 8 + p.part_len - 1) / p.part_len;
   // (tiles of 1024 logits and more: what the last kernel reads of the row once more is a tile)
