@@ -443,6 +443,12 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
 constexpr int kTileKeys = 64, kTilePages = kTileKeys / kBlock;
 
+// 64 lanes x 16 bytes from memory straight into LDS: what lane L reads at from + at lands at `to` + 16 L.  The compiler does not know what
+// it writes (it would wait for it in front of every read of LDS); vmcnt counts it.
+__device__ __forceinline__ void load_to_lds(uint32_t at, const bf16_t* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(at), "s"(from), "s"(to) : "memory", "m0");
+}
+
 // (SHARED: values may lie in a second pool)
 template <int D, int CW, bool SHARED>
 __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFreq inv_freq) {
@@ -488,12 +494,14 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   const size_t block_elems = static_cast<size_t>(a.hkv) * kBlock * D, head_off = static_cast<size_t>(kvh) * kBlock * D;
   const bf16_t *k_pool = static_cast<const bf16_t*>(a.k_pool) + head_off, *v_pool = static_cast<const bf16_t*>(a.v_pool) + head_off;
   const bf16_t* v_shared = static_cast<const bf16_t*>(a.vs.v_shared) + head_off;
-  u32x4 kr[kStage], vr[kStage];
-  // A thread stages the same piece of every 256 / (2 D)-th page, so that page numbers are a wavefront's and addresses a sum with a constant.
+  // A wavefront fetches the same 64 pieces of every 256 / (2 D)-th page straight into LDS, where lane L's piece lands 16 L behind a common address: the
+  // image's order is made by what a lane reads, and page numbers are a wavefront's.
   constexpr int kApart = 128 / D;                                     // pages between a thread's
-  const int pg0 = wave * 64 / (2 * D), piece = tid % (2 * D), token = piece / (D / 8), half = piece & 1;
-  char* const put_k = reinterpret_cast<char*>(image) + ((pg0 * kBlock + token) * (D / 8) + (piece % (D / 8) ^ ((token & 3) | ((token >> 1) & 4)))) * 16;
-  char* const put_v = reinterpret_cast<char*>(image) + (8 * D + pg0 * 2 * D + half * D + ((piece >> 1) ^ (4 * half))) * 16;
+  const int pg0 = wave * 64 / (2 * D), place = tid % (2 * D), half = place / D;          // (place: of the thread's piece in its page's image; half: of the tokens of a V piece)
+  const int token = place / (D / 8);
+  const uint32_t get_k = (token * (D / 8) + (place % (D / 8) ^ ((token & 3) | ((token >> 1) & 4)))) * 16, get_v = (2 * (place % D ^ (4 * half)) + half) * 16;
+  typedef __attribute__((address_space(3))) u32x4 lds_piece;
+  const uint32_t put = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_piece*)image)) + wave * 1024);
   // What the loop needs of the window's tiles, lane t of tile t: where its pages are, and
   //   flag 1: slots of it hold no key of this range,  flag 2: some column of the workgroup does not see all of it
   int w_blk[kTilePages], w_value[SHARED ? kTilePages : 1], w_flags;
@@ -512,18 +520,21 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   auto of_page = [&](const int* w, int j, int t) __attribute__((always_inline)) {       // entry of this wavefront's j-th page of tile t
     return __builtin_amdgcn_readlane(kApart == 1 || pg0 == 0 ? w[kApart * j] : w[kApart * j + kApart - 1], t);
   };
-  auto load = [&](int t) __attribute__((always_inline)) {
+  // tile t into image `buf`
+  auto fetch = [&](int buf, int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < kStage; ++j) {
       const int blk = of_page(w_blk, j, t), value = SHARED ? of_page(w_value, j, t) : blk;
-      kr[j] = *reinterpret_cast<const u32x4*>(k_pool + blk * block_elems + piece * 8);
       const bf16_t* from = !SHARED || value >= 0 ? v_pool + value * block_elems : v_shared + (-1 - value) * block_elems;
-      vr[j] = *reinterpret_cast<const u32x4*>(from + piece * 8);
+      const uint32_t to = put + buf * (kImage * 16) + j * kApart * 32 * D;
+      load_to_lds(get_k, k_pool + blk * block_elems, to);
+      load_to_lds(get_v, from, to + 128 * D);
     }
   };
-  // ... into image `buf`.  Values in slots without a key become zeros (0 x what lies there would be a product).  A tile with values that are not finite
+  // ... until it is there.  Values in slots without a key become zeros (0 x what lies there would be a product).  A tile with values that are not finite
   // and that only some columns see is set aside (odd): 0 x such a value would reach the others.
-  auto store = [&](int buf, int t, int flags, int here) __attribute__((always_inline)) {
+  auto arrive = [&](int buf, int t, int flags, int here) __attribute__((always_inline)) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (flags != 0) {
       bool any = false;
 #pragma unroll
@@ -531,15 +542,11 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
         const int at = kTilePages * t + pg0 + j * kApart, left = (at < here ? list[at].n_valid : 0) - 8 * half;     // of this thread's eight tokens
         auto keep = [&](int e) { return (e < left ? 0xffffu : 0u) | (e + 1 < left ? 0xffff0000u : 0u); };
         auto bad = [](uint32_t v) { return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u; };
-        vr[j] &= u32x4{keep(0), keep(2), keep(4), keep(6)};
-        any |= bad(vr[j][0]) || bad(vr[j][1]) || bad(vr[j][2]) || bad(vr[j][3]);
+        u32x4& v = image[buf * kImage + 8 * D + wave * 64 + lane + j * kApart * 2 * D];
+        v &= u32x4{keep(0), keep(2), keep(4), keep(6)};
+        any |= bad(v[0]) || bad(v[1]) || bad(v[2]) || bad(v[3]);
       }
       if ((flags & 2) && __any(any) && lane == 0) odd[t] = 1;
-    }
-#pragma unroll
-    for (int j = 0; j < kStage; ++j) {
-      *reinterpret_cast<u32x4*>(put_k + buf * (kImage * 16) + j * kApart * 32 * D) = kr[j];
-      *reinterpret_cast<u32x4*>(put_v + buf * (kImage * 16) + j * kApart * 32 * D) = vr[j];
     }
   };
 
@@ -564,7 +571,10 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
   float m = 0.f, l = 0.f;
-  bool begun = false;                                                 // the column has seen a key, m is a reference of its own
+  f32x16 from;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) from[e] = 0.f;
+  float limit = -INFINITY;                                            // how far a logit may be above m: kSlack once the column has seen a key and m is a reference of its own
   // byte of this lane's key operand in an image: row of the block as token of its two pages; piece 2 kk + h is this one's, bits of kk flipped
   const int k_row = (n >> 4) * kBlock + ((n >> 2) & 1) * 8 + ((n >> 3) & 1) * 4 + (n & 3);
   const int k_byte = ((ks * kBlocks * 32 + k_row) * (D / 8) + (h ^ ((k_row & 3) | ((k_row >> 1) & 4)))) * 16, v_byte = (8 * D + ks * kBlocks * 4 * D + h * D + (n ^ (4 * h))) * 16;
@@ -599,12 +609,10 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
       bf16x8 k[kAhead];
 #pragma unroll
       for (int kk = 0; kk < kAhead; ++kk) k[kk] = key(b, kk);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[b][e] = -m;
       fence();
 #pragma unroll
       for (int kk = 0; kk < kSteps; ++kk) {
-        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kk % kAhead], q[kk], s[b], 0, 0, 0);
+        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kk % kAhead], q[kk], kk == 0 ? from : s[b], 0, 0, 0);
         if (kk + kAhead < kSteps) k[kk % kAhead] = key(b, kk + kAhead);
         if constexpr (decltype(under)::value >= 0)
 #pragma unroll
@@ -634,14 +642,16 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
       float top = s[b][0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) top = fmaxf(top, s[b][e]);
-      if (__any(top > kSlack || (!begun && top > -INFINITY))) {
+      if (__ballot(top > limit) != 0) {
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const bool first = !begun && top > -INFINITY;
+        const bool first = limit < 0.f && top > -INFINITY;
         top = first ? top : fmaxf(top, 0.f);                           // how far the reference moves
-        begun |= first;
+        limit = first ? kSlack : limit;
         const float f = first ? 0.f : exp2f(-top);
         m += top;
         l *= f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) from[e] = -m;
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) o[j] *= f;
 #pragma unroll
@@ -744,26 +754,25 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     note_window(here);
     auto flags_of = [&](int t) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(w_flags, t); };
     if (tiles > 0) {
-      load(0);
-      store(0, 0, flags_of(0), here);
-      if (tiles > 1) load(1);
+      fetch(0, 0);
+      arrive(0, 0, flags_of(0), here);
     }
     __syncthreads();
     bool aside = false;                                               // (of this window some tile)
     for (int t = 0; t < tiles; ++t) {
-      if (t + 1 < tiles) store((t + 1) & 1, t + 1, flags_of(t + 1), here);
-      if (t + 2 < tiles) load(t + 2);
+      if (t + 1 < tiles) fetch((t + 1) & 1, t + 1);
       const int flags = flags_of(t);
       const bool skip = (flags & 2) != 0 && __builtin_amdgcn_readfirstlane(odd[t]) != 0;
       aside |= skip;
       if (!skip) compute(std::false_type(), image + (t & 1) * kImage, t * kTilePages, here, flags);
+      if (t + 1 < tiles) arrive((t + 1) & 1, t + 1, flags_of(t + 1), here);
       __syncthreads();
     }
     if (aside)
       for (int t = 0; t < tiles; ++t)
         if (odd[t] != 0) {
-          load(t);
-          store(0, t, flags_of(t), here);
+          fetch(0, t);
+          arrive(0, t, flags_of(t), here);
           __syncthreads();
           compute(std::true_type(), image, t * kTilePages, here, flags_of(t));
           __syncthreads();
@@ -772,7 +781,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
 
   // ---- results
   l += __shfl_xor(l, 32, 64);
-  m = begun ? m : -3.4028235e38f;
+  m = limit < 0.f ? -3.4028235e38f : m;
   float* mine = reinterpret_cast<float*>(image);
   if constexpr (KS == 2) {
     // the second stream's sums go through LDS to the first one's lanes: [value][lane]
