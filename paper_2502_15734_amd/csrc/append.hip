@@ -437,9 +437,9 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
 // v_mfma_f32_32x32x16_bf16, S^T = K Q^T and O^T = V^T P^T with lane = (n = lane % 32, h = lane / 32), column n.  As above the key rows are
 // ordered so that a lane's logits are the tokens 8 h .. 8 h + 7 of each page: row 8 a + 4 b + c of a 32-key block is token
 // 8 b + 4 (a % 2) + c of page a / 2.  Image (16-byte pieces):
-//   K  token t of the tile, piece ch of its row:        t * D / 8 + (ch ^ f(t)),  f(t) = t % 4 + 4 (t / 8 % 2)
+//   K  token t of the tile, piece ch of its row:        t * D / 8 + (ch ^ f(t)),  f(t) = t % 16, or t / 2 % 8 if D is 64
 //   V  page, dim d, half h of its row of 16 tokens:     8 D + page * 2 D + h * D + (d ^ 4 h)
-// (eight lanes of a read or write meet eight different 16-byte columns of the banks)
+// (sixteen lanes of a read meet the sixteen 16-byte columns of the banks)
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
 constexpr int kTileKeys = 64, kTilePages = kTileKeys / kBlock;
 
@@ -499,7 +499,8 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   constexpr int kApart = 128 / D;                                     // pages between a thread's
   const int pg0 = wave * 64 / (2 * D), place = tid % (2 * D), half = place / D;          // (place: of the thread's piece in its page's image; half: of the tokens of a V piece)
   const int token = place / (D / 8);
-  const uint32_t get_k = (token * (D / 8) + (place % (D / 8) ^ ((token & 3) | ((token >> 1) & 4)))) * 16, get_v = (2 * (place % D ^ (4 * half)) + half) * 16;
+  auto turn = [](int t) { return D == 128 ? t & 15 : (t >> 1) & 7; };
+  const uint32_t get_k = (token * (D / 8) + (place % (D / 8) ^ turn(token))) * 16, get_v = (2 * (place % D ^ (4 * half)) + half) * 16;
   typedef __attribute__((address_space(3))) u32x4 lds_piece;
   const uint32_t put = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_piece*)image)) + wave * 1024);
   // What the loop needs of the window's tiles, lane t of tile t: where its pages are, and
@@ -577,7 +578,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   float limit = -INFINITY;                                            // how far a logit may be above m: kSlack once the column has seen a key and m is a reference of its own
   // byte of this lane's key operand in an image: row of the block as token of its two pages; piece 2 kk + h is this one's, bits of kk flipped
   const int k_row = (n >> 4) * kBlock + ((n >> 2) & 1) * 8 + ((n >> 3) & 1) * 4 + (n & 3);
-  const int k_byte = ((ks * kBlocks * 32 + k_row) * (D / 8) + (h ^ ((k_row & 3) | ((k_row >> 1) & 4)))) * 16, v_byte = (8 * D + ks * kBlocks * 4 * D + h * D + (n ^ (4 * h))) * 16;
+  const int k_byte = ((ks * kBlocks * 32 + k_row) * (D / 8) + (h ^ turn(k_row))) * 16, v_byte = (8 * D + ks * kBlocks * 4 * D + h * D + (n ^ (4 * h))) * 16;
 
   // One tile.  ODD: one that was set aside.  i: its first entry of the list, of which `here` count.
   // In the order  S(0), S(1) with the exponentials of block 0 under its products, P V(0) with those of block 1, P V(1), four operands read ahead; the
