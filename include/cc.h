@@ -465,7 +465,8 @@ int cc_chunk_attention(cc_ctx* ctx, const void* q, const int32_t* q_pos, const i
 /* ---- (f) tables of new rows -------------------------------------------------------------------
  * Every segment s of the batch holds segs_in[s].n_tokens tokens (their keys and values are in its pages) and
  * gets n_new[s] more behind them (negative: none).  A segment in front of others of its request may grow only while
- * those are empty (the positions of what is cached are fixed).  From nothing (n_tokens = 0, n_new = the lengths)
+ * those are empty (the positions of what is cached are fixed).  req_seg_off ascends from 0 to n_segs; the segments' own
+ * req is not read.  From nothing (n_tokens = 0, n_new = the lengths)
  * the call lays out whole prompts; with one new token in each request's last segment it is a step of an answer.
  *   segs [n_segs]: segs_in (may be the same array) with
  *       req = the request r whose [req_seg_off[r], req_seg_off[r + 1]) holds s,  n_tokens = old + new,
@@ -478,7 +479,7 @@ int cc_chunk_attention(cc_ctx* ctx, const void* q, const int32_t* q_pos, const i
  *   cu_q [n_requests + 1]: row offsets of the requests.  For row j < cu_q[n_requests], in the order of the
  *       segments and their tokens:  q_pos[j] = position, slot_map[j] = page * 16 + t % 16 of token t of its segment
  *       (-1 if the page is not in [0, n_blocks)), row_req[j] = request;  for the rows behind, up to max_rows
- *       (the size of the three arrays): 0, -1, -1, so that a call over max_rows rows writes nothing for them.
+ *       (the size of the three arrays, at most 2^30): 0, -1, -1, so that a call over max_rows rows writes nothing for them.
  *   last_row [n_requests]: the request's last row, -1 if it has none (the row whose logits are sampled).
  *   status [n_requests]: CC_EXTEND_OK, or why the request gets NOTHING in this call: a segment's entries do not
  *       hold its pages (or the request would reach 2^31 tokens), a segment in front of cached tokens grows,
@@ -499,11 +500,14 @@ int cc_extend_segments(cc_ctx* ctx, const cc_segment* segs_in, const int32_t* n_
  * checked at once, some hundred for a further question over a long context.  The same two steps and the same
  * arguments (rows, positions and slots from cc_extend_segments or any list cc_sparse_prefill takes), but the KEYS are
  * divided over workgroups, and the parts joined, so that a few rows of a long context fill the chip.
- *   Rows [cu_q[n_requests], n_q_tot) are not attended and their out and lse stay as they are; rows whose slot lies
- *   outside the pool are attended but not written.  A row that sees no key gets zeros and lse = -infinity.
+ *   slot_map[j] is the slot of row j's own token, in a page of its request, or lies outside the pool: the row is then
+ *   attended but not written.  Rows [cu_q[n_requests], n_q_tot) are not attended, their out and lse stay as they are, and
+ *   their slots lie outside the pool (cc_extend_segments leaves them so).  A row that sees no key gets zeros and
+ *   lse = -infinity.
  *   What lies in a masked place (padding slots, keys behind the row, pages outside the pool) changes nothing, NaN
  *   and infinities included.
- *   max_q_per_req: at least the rows of any request (host scalar; bounds the grid).
+ *   max_q_per_req: at least the rows of any request (host scalar; bounds the grid: a call that would need 2^24 workgroups
+ *   or more is refused).
  *   max_ctx_tokens, max_segs_per_req: tokens and segments of the largest request (host scalars, upper bounds; they
  *   decide how the keys are divided, not what is read).  lse may be NULL; shared as for cc_sparse_prefill.
  *   The sums' order depends on n_requests, max_q_per_req, max_ctx_tokens and max_segs_per_req, on nothing else.
@@ -532,7 +536,8 @@ int cc_append_attention(cc_ctx* ctx, const void* q, const void* k_new, const voi
  * -infinity and NaN are never kept; a row of nothing else gives token -1, logprob -infinity, n_kept 0.  Beside +infinity
  * every finite logit has weight 0.  u below 0 or NaN counts as 0, u of 1 or more as the largest float below 1.
  * NULL turns off: temperature (1 then), top_k, top_p, min_p, logprob, n_kept.  All [n_rows].
- * Weights are taken in 64 bits and summed as whole numbers, so that the result does not depend on how the work is divided.
+ * Weights are taken in 64 bits and summed as whole multiples of 2^-s, s = min(50, 62 - ceil(log2 n_vocab)) (45 at 128256
+ * columns), so that the result does not depend on how the work is divided; a weight below 2^-(s + 1) counts as 0.
  *   workspace: cc_sample_workspace_bytes(ctx, n_rows, n_vocab). */
 size_t cc_sample_workspace_bytes(const cc_ctx* ctx, int32_t n_rows, int32_t n_vocab);
 int cc_sample(cc_ctx* ctx, const void* logits, int32_t logits_dtype, int32_t n_rows, int32_t n_vocab, int64_t stride,

@@ -657,6 +657,7 @@ int cc_extend_segments(cc_ctx* ctx, const cc_segment* segs_in, const int32_t* n_
   CC_REQUIRE(n_segs >= 0 && n_requests >= 0 && n_free >= 0 && n_tab >= 0 && n_blocks >= 0 && max_rows >= 0, "negative count");
   CC_REQUIRE(n_segs <= 65535 && n_requests <= 65535, "more than 65535 segments or requests in one call");
   CC_REQUIRE(n_blocks <= (1 << 27) - 1, "a pool of more than 2^27 - 1 blocks has slots beyond 32 bits");
+  CC_REQUIRE(max_rows <= (1 << 30), "more than 2^30 rows in one call");
   if (n_requests == 0) return CC_OK;
   CC_REQUIRE(req_seg_off && cu_q && last_row && status && counts, "null pointer");
   CC_REQUIRE(n_segs == 0 || (segs_in && segs && n_new && tab_cap), "null pointer");
@@ -697,6 +698,8 @@ int cc_append_attention(cc_ctx* ctx, const void* q, const void* k_new, const voi
   CC_REQUIRE(aligned16(q) && aligned16(k_new) && aligned16(v_new) && aligned16(k_pool) && aligned16(v_pool) && aligned16(out) && aligned16(segs),
              "tensors must be 16-byte aligned");
   CC_REQUIRE(q != out, "q and out must not be the same tensor");
+  CC_REQUIRE(cc::append_groups(ctx, max_q_per_req, n_requests, max_ctx_tokens, max_segs_per_req) < (1 << 24),
+             "more than 2^24 - 1 workgroups: max_q_per_req x n_requests is too large for one call");
   const size_t need = cc_append_attention_workspace_bytes(ctx, n_q_tot, max_q_per_req, n_requests, max_ctx_tokens, max_segs_per_req);
   CC_REQUIRE(need == 0 || (workspace != nullptr && aligned16(workspace)), "workspace missing or misaligned");
   if (workspace_bytes < need)

@@ -963,6 +963,10 @@ __global__ __launch_bounds__(64) void append_scalar_kernel(
   if (lse != nullptr && lane == 0) lse[static_cast<size_t>(j) * hq + h] = z == 0.f ? -INFINITY : m + logf(z);
 }
 
+long long append_groups(const cc_ctx* ctx, int max_q_per_req, int n_requests, int max_ctx_tokens, int max_segs_per_req) {
+  return plan_append(ctx, max_q_per_req, n_requests, max_ctx_tokens, max_segs_per_req).groups;
+}
+
 size_t append_bytes(const cc_ctx* ctx, int n_q_tot, int max_q_per_req, int n_requests, int max_ctx_tokens, int max_segs_per_req) {
   if (ctx->impl == CC_IMPL_SCALAR || n_q_tot == 0) return 0;
   const AppendPlan p = plan_append(ctx, max_q_per_req, n_requests, max_ctx_tokens, max_segs_per_req);

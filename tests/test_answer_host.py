@@ -111,3 +111,16 @@ def test_refused_arguments(lib):
     if need:
         assert call(bytes=need - 1) == -3 and call(ws=None) == -1 and call(ws=odd) == -1
     ctx.close()
+
+
+def test_calls_beyond_the_grid_are_refused(lib):
+    """Rows and workgroups that a launch could not count are refused, not cut off."""
+    import paper_2502_15734_amd as P
+    ctx = P.Context(8, 2, 128, 5.0e5, P.CC_BF16)
+    h, good = ctx._h, C.c_void_p(4096)
+    assert lib.cc_extend_segments(h, good, good, good, 1, good, 1, good, 4, good, 9, 8, good, good, good, good, good, (1 << 30) + 1, good, good, good,
+                                  good, 1 << 30, None) == -1 and b"2^30 rows" in lib.cc_last_error(h)
+    # 65535 requests of up to 2^17 rows: 2 KV heads x 2^17 x 4 / 128 column groups each
+    assert lib.cc_append_attention(h, good, good, good, None, good, good, good, 1 << 18, 1 << 17, good, good, 8, good, good, 65535, good, 65535, 4000, 1,
+                                   None, C.c_void_p(8192), None, good, 1 << 60, None) == -1 and b"2^24 - 1 workgroups" in lib.cc_last_error(h)
+    ctx.close()
