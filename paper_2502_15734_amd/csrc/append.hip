@@ -882,7 +882,14 @@ __global__ __launch_bounds__(256) void append_join_kernel(AppendArgs a, int n_it
   store_result<T, D>(a, at, 0, 1, 4 * lane, v, top, sum);
 }
 
-// How the work of a call is divided: from host scalars alone.
+// How the work of a call is divided: from host scalars alone.  What either side of a choice takes (16 requests of 1000 to 8000 tokens, 64 heads on 8, if
+// nothing else is said):
+//   columns of a workgroup   up to 16: append_split_kernel; 32 columns as two groups of it 112 us, as one of 64 columns of append_tile_kernel 78.
+//                            up to 64, then 128: 72 columns as two groups of 64 116 us, as one of 128 87
+//   ranges                   about 512 workgroups, two on a compute unit: the tile kernel with 256 97 us, with 512 76, with 1024 92; the split kernel 70, 73, 82
+//                            (and 32 requests of one row 118, 115, 125).  The split kernel's number is the nearest, the tile kernel's rounded down: 24
+//                            requests with 1.3 workgroups a unit 83 us, with 2 70; 40 requests of 8 rows with 1.25 145 us, with 2.5 164
+//   pages of a range         at least 8 (16 for a tile): 8 rows over 8000 tokens with 4 26 us, with 8 23, with 16 24.4
 struct AppendPlan {
   int cols;                           // columns of a workgroup: 16 (append_split_kernel); 64, 128 (append_tile_kernel)
   int col_groups, n_splits, split_pages;
@@ -894,8 +901,8 @@ AppendPlan plan_append(const cc_ctx* ctx, int max_q_per_req, int n_requests, int
   p.cols = cols <= 16 || ctx->cfg.dtype != CC_BF16 ? 16 : cols <= 64 ? 64 : 128;
   p.col_groups = static_cast<int>((cols + p.cols - 1) / p.cols);
   const long long pages = max_ctx_tokens / kBlock + static_cast<long long>(max_segs_per_req), units = static_cast<long long>(ctx->cfg.n_kv_heads) * n_requests;
-  const long long target = 512, least = p.cols == 16 ? 8 : 16;
-  const long long splits = std::max(1ll, std::min(target / std::max(1ll, units * p.col_groups), (pages + least - 1) / least));
+  const long long target = 512, least = p.cols == 16 ? 8 : 16, all = std::max(1ll, units * p.col_groups);
+  const long long splits = std::max(1ll, std::min((p.cols == 16 ? target + all / 2 : target) / all, (pages + least - 1) / least));
   p.split_pages = static_cast<int>(((pages + splits - 1) / splits + 3) & ~3ll);
   p.n_splits = static_cast<int>((pages + p.split_pages - 1) / p.split_pages);
   p.groups = (units * p.n_splits + 7) / 8 * 8 * p.col_groups;
