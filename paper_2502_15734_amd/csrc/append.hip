@@ -12,7 +12,13 @@
 // logits of tokens 8 (g % 2) .. + 7 of page g / 2: as the second product's 32-token operand they meet a 16-byte piece of a
 // dimension-major V row.  fp32, a tile of one page: steps of four tokens, as in qk_f32.hip.
 //
-// The softmax reference of a column is shared by the four lane groups and moves only when a logit is more than kSlack above it.
+// One pass: o = sum_t 2^(s_t - m) v_t and l = sum_t 2^(s_t - m), where the reference m of a column is shared by its lane groups and moves (o and l times
+// 2^(old - new)) only when a logit is more than kSlack above it.  m, l and o are fp32; queries, once they are turned to their position, and weights are rounded
+// to the element type, which is what the matrix instructions take.
+//
+// 32 heads on 8 of 128, bf16: 32 requests of one row over 1500 to 6700 tokens 115 us (4.5 TB/s of keys and values; a copy of 4 GiB moves 4.7), one
+// row over 130 000 tokens 104 us (5.1 TB/s), one over 700 tokens 12.2 us, of which two launches take 5 and the chain of dependent loads (segments, page
+// table, page, parts) most of the rest.
 #include <algorithm>
 #include <type_traits>
 
@@ -429,10 +435,13 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
 }
 
 // ---- many columns -------------------------------------------------------------------------------
-// A draft to check or a further question: 33 columns and more (rows times heads of a group) share the keys.  Workgroup = 32 CW columns x a range
-// of pages; tiles of 64 keys go through LDS (registers hold the next tile, two images, one barrier per tile), so that a page is read
+// A draft to check or a further question: 17 columns and more (rows times heads of a group) share the keys.  Workgroup = 32 CW columns x a range
+// of pages; tiles of 64 keys go through LDS (two images, loads that write LDS while the other is multiplied, one barrier per tile), so that a page is read
 // once for all its columns.  CW = 4: each wavefront multiplies its 32 columns with all 64 keys; CW = 2: two wavefronts per 32 columns take 32
-// keys each and meet at the end.  Bound by the matrix cores and the exponentials beside them from some hundred columns on.
+// keys each and meet at the end.  Few columns are bound by the bytes (16 requests of 5 rows over 1000 to 8000 tokens, 64 heads on 8: 78 us, 3.7 TB/s), from some
+// hundred on by the vector instructions beside the matrix instructions: 500 rows of 32 heads over 16 000 tokens take 165 us, of them 150 in this
+// kernel, with the matrix cores busy for half of its cycles, LDS for a quarter, and the rest in what lies between two products of a tile (maximum, mask,
+// barrier) that the other workgroup of the compute unit does not cover.
 //
 // v_mfma_f32_32x32x16_bf16, S^T = K Q^T and O^T = V^T P^T with lane = (n = lane % 32, h = lane / 32), column n.  As above the key rows are
 // ordered so that a lane's logits are the tokens 8 h .. 8 h + 7 of each page: row 8 a + 4 b + c of a 32-key block is token
@@ -819,6 +828,8 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
 
 // Joins the ranges of a row and head: sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  D / 4 threads take four dims each; where there are many
 // ranges (WIDE) the groups of such threads of a workgroup share one row and head, every so-manieth range each, otherwise they take one each.
+// Bound by the parts it reads: 500 rows of 32 heads in 4 ranges, 33 MB, 8 us; 16 x 5 rows of 64 heads in 4, 10 MB, 5 us; a few rows take a launch and two
+// trips to memory, 2.5 to 4 us.  (8 rows over 8000 tokens, 63 ranges: WIDE 22.8 us of the whole call, otherwise 25.1; up to 8 ranges there is no difference.)
 template <typename T, int D, bool WIDE>
 __global__ __launch_bounds__(256) void append_join_kernel(AppendArgs a, int n_items) {
   constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
@@ -1017,7 +1028,7 @@ void launch_append_attention(const cc_ctx* ctx, const void* q, const int32_t* sr
     return;
   }
   const AppendPlan p = plan_append(ctx, max_q_per_req, n_requests, max_ctx_tokens, max_segs_per_req);
-  // Few rows are written by the workgroups that read them, which saves a launch (5 to 9 us); not into pages whose values may still be in
+  // Few rows are written by the workgroups that read them, which saves a launch (one row over 2000 tokens 13.2 us instead of 17.8, 16 x 9 rows of 64 heads 87 instead of 92); not into pages whose values may still be in
   // the chunk store: those are copied whole, for all KV heads at once.
   const bool write = p.col_groups == 1 && max_q_per_req <= kWriteRows && vs.v_map == nullptr;
   if (!write) launch_rope_scatter(ctx, scatter, stream);
