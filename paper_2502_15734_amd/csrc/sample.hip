@@ -304,6 +304,7 @@ struct Cuts {
   unsigned count_lo, count_hi;        // tokens in front of p_lo, behind p_hi
   unsigned count_k;                   // tokens in front of k_bin
   unsigned listed;                    // candidates
+  unsigned unlisted;                  // tokens of the last bin that pass top-k and have no weight: they count as kept, which of them does not matter
   unsigned long long mass_lo, mass_k, mass_all;      // weights in front of p_lo, of k_bin, of all bins
 };
 
@@ -384,9 +385,10 @@ __device__ __forceinline__ Part row_extremes(const RowScratch& ws, int parts) {
 // the bins are in that order and equal logits share one.
 struct Bins {
   float top, per;
-  bool usable;
+  bool usable, far;                   // far: the last bin holds nothing else than weights below 2^-66, zeros of the sums
   __device__ __forceinline__ Bins(float top_, float low, double inv_t) : top(top_) {
-    const float span = fminf(top - low, static_cast<float>(46.0 / inv_t));
+    const float most = static_cast<float>(46.0 / inv_t), span = fminf(top - low, most);
+    far = most < top - low;
     per = span > 0.f ? kBins / span : 0.f;
     usable = span < INFINITY && per < INFINITY;
   }
@@ -396,7 +398,7 @@ struct Bins {
 // Where the cuts fall, from the histogram.  With both top-k and top-p the weight that top-p refers to is known to the bin that top-k's cut
 // falls into, so top-p's has a first and a last possible bin.
 template <int N>
-__device__ __forceinline__ Cuts find_cuts(const RowScratch& ws, const RowSettings& s) {
+__device__ __forceinline__ Cuts find_cuts(const RowScratch& ws, const RowSettings& s, bool far) {
   constexpr int kOwn = kBins / N;     // bins of a thread
   __shared__ unsigned long long wave_mass[N / 64];
   __shared__ unsigned wave_count[N / 64];
@@ -429,7 +431,7 @@ __device__ __forceinline__ Cuts find_cuts(const RowScratch& ws, const RowSetting
     mass_all += wave_mass[w];
   }
   const bool by_k = static_cast<unsigned>(s.top_k) < count_all, by_p = s.top_p < 1.0;
-  if (tid == 0) cuts = Cuts{kBins, kBins, kBins, count_all, count_all, count_all, 0, mass_all, mass_all, mass_all};
+  if (tid == 0) cuts = Cuts{kBins, kBins, kBins, count_all, count_all, count_all, 0, 0, mass_all, mass_all, mass_all};
   __syncthreads();
   // (f(bin, tokens in front, weights in front, with the bin's own) for this thread's bins)
   auto each = [&](auto&& f) __attribute__((always_inline)) {
@@ -464,7 +466,17 @@ __device__ __forceinline__ Cuts find_cuts(const RowScratch& ws, const RowSetting
   }
   __syncthreads();
   Cuts out = cuts;
-  out.listed = out.count_hi - out.count_lo + (out.k_bin > out.p_hi ? count_with_k - out.count_k : 0u);
+  // top-k reaches into logits that were masked by a low number: no list of thousands of equal ones for that
+  if (far && out.k_bin == kBins - 1 && !(s.min_p > 0.0 && s.min_p < 0x1p-60)) {
+    if (!by_p) {
+      out.unlisted = s.min_p > 0.0 ? 0u : static_cast<unsigned>(s.top_k) - out.count_k;
+      out.p_lo = kBins - 1;
+      out.p_hi = kBins - 2;
+      out.count_hi = out.count_lo;
+    }
+    if (!by_p || out.p_hi < kBins - 1) out.k_bin = kBins;
+  }
+  out.listed = out.count_hi - out.count_lo + (out.k_bin < kBins && out.k_bin > out.p_hi ? count_with_k - out.count_k : 0u);
   return out;
 }
 
@@ -557,7 +569,7 @@ __global__ __launch_bounds__(256) void sample_tiles_kernel(SampleArgs a, SampleP
   __syncthreads();
   int p_lo = kBins, p_hi = kBins, k_bin = kBins;
   if (cut) {
-    const Cuts c = find_cuts<256>(ws, s);
+    const Cuts c = find_cuts<256>(ws, s, bins.far);
     if (part == 0 && tid == 0) ws.cuts = c;
     if (c.listed > kList) return;                      // (the last kernel does the row alone)
     p_lo = c.p_lo; p_hi = c.p_hi; k_bin = c.k_bin;
@@ -707,7 +719,7 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
   uint32_t top;
   int top_idx;
   Part x{0, 0, 0, 0};
-  Cuts c{0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+  Cuts c{};
   int n_list = 0;
   bool whole = false;                                  // the list does not hold the candidates
   // (what the other kernels left, in one trip to memory; what this row does not use is not looked at)
@@ -831,7 +843,7 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
   // ---- the tile the number falls into
   const unsigned long long here = tid < n_tiles ? sh.list.tile[tid] : 0ull;
   const unsigned long long front = block_before<W>(here, part_mass), total = block_sum<W>(here, part_mass);
-  const unsigned n_kept = block_sum<W>(tile_kept, part_count) + kept_list;
+  const unsigned n_kept = block_sum<W>(tile_kept, part_count) + kept_list + (parts && cut ? c.unlisted : 0u);
   const double target = s.u * static_cast<double>(total);
   if (static_cast<double>(front) <= target && static_cast<double>(front + here) > target) { found = tid; found_before = front; }
   __syncthreads();

@@ -476,6 +476,24 @@ def test_sample_ties(vocab, dtype):
         _check_sample(_sample(_ctx(), z, vocab, u, **s), z, vocab, u, **s)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [900, 20000, 128256])
+def test_sample_masked_by_the_lowest_value(vocab, dtype):
+    """All but a few tokens at the type's lowest value, and top-k beyond the few: the masked ones count as kept, and are never drawn."""
+    kind, rng, rows = torch.bfloat16 if dtype == "bf16" else torch.float32, np.random.default_rng(vocab), 10
+    z = torch.full((rows, vocab), torch.finfo(kind).min)
+    for r in range(rows):
+        at = torch.from_numpy(rng.choice(vocab, 3 + 9 * r, replace=False))
+        z[r, at] = torch.from_numpy(rng.standard_normal(len(at)).astype(np.float32)) * 3
+    z = z.to(kind).cuda()
+    k, full = np.full(rows, 50), np.ones(rows)
+    heat = rng.uniform(0.2, 2.0, rows)
+    for s in (dict(top_k=k), dict(top_k=k * 3, temperature=heat), dict(top_k=k, top_p=0.9 * full, temperature=heat), dict(top_k=k, min_p=0.01 * full),
+              dict(top_k=k, top_p=0.9999999 * full), dict(top_k=k, min_p=1e-30 * full), dict(top_p=0.8 * full), dict(top_k=np.full(rows, vocab - 1), temperature=heat)):
+        for u in (rng.random(rows, dtype=np.float32), np.full(rows, 1 - 2.0 ** -24, np.float32)):
+            _check_sample(_sample(_ctx(), z, vocab, u, **s), z, vocab, u, **s)
+
+
 @pytest.mark.parametrize("vocab", [200, 9000])
 def test_sample_values_that_are_not_finite(vocab):
     rng = np.random.default_rng(vocab)
