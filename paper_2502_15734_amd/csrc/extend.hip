@@ -7,6 +7,8 @@
 // Bound by latency: a step of some hundred answers reads and writes some ten kilobytes, and a launch costs more than that.  So batches
 // whose tables fit a workgroup's LDS are one launch of one workgroup (extend_small_kernel); others are a launch for the needs, one that
 // places the segments (every workgroup scans all needs again, which is cheaper than a launch between) and one for the rows.
+// 32 requests of one row each (5 to 10 segments) 7.5 us, where a launch alone takes 2.4; 250 requests, some with a question, 13.8; the tables of 500 whole
+// prompts, 2.8 million rows, 22 us (1.6 TB/s, of which a third is the chain through the two kernels in front).
 #include "device_util.h"
 
 namespace cc {
@@ -467,7 +469,8 @@ __global__ __launch_bounds__(64 * W) void extend_small_kernel(ExtendArgs a) {
   }
 }
 
-// Wavefronts of the workgroup that does it alone; 0: the tables are too large for one.
+// Wavefronts of the workgroup that does it alone; 0: the tables are too large for one.  (32 requests: 4 wavefronts 7.5 us, 16 9.7, three launches 14.9; 250
+// requests with 1600 segments: 16 wavefronts 13.8, three launches 18.1)
 int small_waves(int n_segs, int n_requests, int max_rows) {
   for (int w : {4, 16})
     if (n_segs <= 64 * w * kOwn && n_requests <= 64 * w && max_rows <= 64 * w * kOwnRows) return w;

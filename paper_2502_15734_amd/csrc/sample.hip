@@ -14,7 +14,12 @@
 //                        logits of that bin, the candidates
 //   sample_draw_kernel   sorts the candidates, finds the cut among them, the tile the drawn number falls into and the token in it
 // Rows with more candidates than the list holds (thousands of equal logits) are done by the last kernel alone, with radix descents
-// over the whole row; vocabularies that fit the list need no other kernel than the last.
+// over the whole row (32000 equal ones 0.6 ms, 128256 2 ms); vocabularies that fit the list need no other kernel than the last.
+//
+// Few rows are bound by latency: four launches, each with a chain of two or three loads, scans and barriers (1 x 32000 fp32 with top-p 23.6 us, of
+// which the last kernel takes 8; 32 x 128256 bf16 36 us).  Many rows are bound by the three reads and the arithmetic in 64 bits beside the second and third:
+// 256 x 128001 fp32 (131 MB) with all kinds of settings 106 us: 26 for the first pass (5 TB/s), 26, 36 and 13 to 25 for the last kernel, the
+// longest where a row has many candidates to sort.
 #include <algorithm>
 
 #include "device_util.h"
@@ -873,7 +878,9 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
     }
 }
 
-// Parts of at least 2048 logits, so many that a call has about a thousand workgroups (four on a compute unit), at most 64 a row.
+// Parts of 2048 to 8192 logits, so many that a call has about a thousand workgroups (four on a compute unit), at most 64 a row.  32 x 128256 with 1024
+// workgroups 36 us, with 512 or 2048 43; 256 x 128001 in parts of 8192 113 us, of 4096 or 16384 126 (rows differ in work: shorter parts even it
+// out, and each part has its cuts to find).  Workgroups of 16 wavefronts took longer throughout (1 x 32000 27.7 us instead of 23.5, 64 x 128256 57 instead of 49).
 SamplePlan sample_plan(int n_rows, int vocab) {
   SamplePlan p{0, 0, 0, 0};
   if (vocab <= kList) return p;
@@ -900,7 +907,7 @@ static void launch_sample_t(const SampleArgs& a, const SamplePlan& plan, RowScra
     if (a.top_k != nullptr || a.top_p != nullptr) hipLaunchKernelGGL(sample_hist_kernel<T>, grid, dim3(256), 0, stream, a, plan, ws);
     hipLaunchKernelGGL(sample_tiles_kernel<T>, grid, dim3(256), 0, stream, a, plan, ws);
   }
-  // (behind other kernels a workgroup of four wavefronts: its barriers and sums over wavefronts are most of its time)
+  // (behind other kernels a workgroup of four wavefronts: its barriers and sums over wavefronts are most of its time, and four of them have fewer)
   if (plan.parts > 0) hipLaunchKernelGGL((sample_draw_kernel<T, 4>), dim3(a.n_rows), dim3(256), 0, stream, a, plan, ws);
   else hipLaunchKernelGGL((sample_draw_kernel<T, 16>), dim3(a.n_rows), dim3(1024), 0, stream, a, plan, ws);
 }
