@@ -155,6 +155,7 @@ template <typename T, int D> struct Tile;           // operands of one tile of k
 
 template <int D> struct Tile<bf16_t, D> {
   static constexpr int kPages = 2, kTok = 8;        // pages of a tile; tokens of it that a lane holds
+  static constexpr int kParts = 2;                  // of queries and weights, whose sum has 16 bits of them: the bytes of the keys bound this kernel, not its products
   typedef bf16x8 Piece;
   Piece k[2][D / 32], v[D / 16];
   static __device__ __forceinline__ int page_of(int lane) { return lane >> 5; }                // of the tokens the lane holds
@@ -172,29 +173,36 @@ template <int D> struct Tile<bf16_t, D> {
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) v[i] = *reinterpret_cast<const Piece*>(vp + i * 16 * kBlock);
   }
-  __device__ __forceinline__ void logits(const Piece (&q)[D / 32], float (&s)[kTok]) const {
+  __device__ __forceinline__ void logits(const Piece (&q)[kParts][D / 32], float (&s)[kTok]) const {
     f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][i], q[i], acc[t], 0, 0, 0);
+      for (int x = 0; x < kParts; ++x)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][i], q[x][i], acc[t], 0, 0, 0);
 #pragma unroll
     for (int e = 0; e < kTok; ++e) s[e] = acc[e >> 2][e & 3];
   }
   static __device__ __forceinline__ f32x4 add_values(const Piece& v, const Piece& p, f32x4 o) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o, 0, 0, 0);
   }
-  // (queries and weights: their one rounding, as the matrix instruction takes bf16)
-  static __device__ __forceinline__ Piece piece(const float (&x)[8]) {
+  // Part 0: the upper 16 bits, x becomes the rest; part 1: the nearest to that.  The rest keeps the sign and is not 0, so that a product with an infinite
+  // factor is one infinity and not a difference of two.
+  static __device__ __forceinline__ Piece piece(float (&x)[8], int part) {
     Piece w;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = static_cast<bf16_t>(x[e]);
+    for (int e = 0; e < 8; ++e) {
+      const float up = __uint_as_float(__float_as_uint(x[e]) & (part == 0 ? 0xffff0000u : 0xffffffffu));
+      w[e] = static_cast<bf16_t>(up);
+      x[e] = copysignf(fmaxf(fabsf(x[e] - up), 0x1p-126f), up);
+    }
     return w;
   }
 };
 
 template <int D> struct Tile<float, D> {
-  static constexpr int kPages = 1, kTok = 4;
+  static constexpr int kPages = 1, kTok = 4, kParts = 1;
   typedef f32x4 Piece;
   Piece k[1][D / 16], v[D / 16];
   static __device__ __forceinline__ int page_of(int) { return 0; }
@@ -211,14 +219,14 @@ template <int D> struct Tile<float, D> {
     for (int i = 0; i < D / 16; ++i) v[i] = *reinterpret_cast<const Piece*>(vp + i * 16 * kBlock);
   }
   // (four chains of additions: one of D would lose two bits)
-  __device__ __forceinline__ void logits(const Piece (&q)[D / 16], float (&s)[kTok]) const {
+  __device__ __forceinline__ void logits(const Piece (&q)[kParts][D / 16], float (&s)[kTok]) const {
     f32x4 acc[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[0][i][e], q[i][e], acc[e], 0, 0, 0);
+      for (int e = 0; e < 4; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[0][i][e], q[0][i][e], acc[e], 0, 0, 0);
 #pragma unroll
     for (int e = 0; e < kTok; ++e) s[e] = (acc[0][e] + acc[1][e]) + (acc[2][e] + acc[3][e]);
   }
@@ -227,7 +235,7 @@ template <int D> struct Tile<float, D> {
     for (int e = 0; e < 4; ++e) o = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], p[e], o, 0, 0, 0);
     return o;
   }
-  static __device__ __forceinline__ Piece piece(const float (&x)[4]) { return Piece{x[0], x[1], x[2], x[3]}; }
+  static __device__ __forceinline__ Piece piece(const float (&x)[4], int) { return Piece{x[0], x[1], x[2], x[3]}; }
 };
 
 // What a workgroup does.  Workgroups go to the eight XCDs in turn; the column groups of one range of keys, which read the same pages, follow
@@ -280,14 +288,14 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
 
   // ---- positions of the columns, and the rows themselves (loads first, turned later)
   // (columns behind the last repeat its row)
-  Piece q[kQ];
+  Piece q[Keys::kParts][kQ];
   const int my_col = min(col0 + n, n_cols - 1), pos = a.q_pos[row0 + my_col / group];
   {
     const int row = row0 + my_col / group;
     const int src = a.src_rows != nullptr ? a.src_rows[row] : row;
     const T* qp = static_cast<const T*>(a.q) + (static_cast<size_t>(src) * a.hq + kvh * group + my_col % group) * D + kPer * g;
 #pragma unroll
-    for (int i = 0; i < kQ; ++i) q[i] = *reinterpret_cast<const Piece*>(qp + 4 * kPer * i);
+    for (int i = 0; i < kQ; ++i) q[0][i] = *reinterpret_cast<const Piece*>(qp + 4 * kPer * i);
   }
   const size_t block_elems = static_cast<size_t>(a.hkv) * kBlock * D, head_off = static_cast<size_t>(kvh) * kBlock * D;
   const T *k_pool = static_cast<const T*>(a.k_pool), *v_pool = static_cast<const T*>(a.v_pool), *v_shared = static_cast<const T*>(a.vs.v_shared);
@@ -313,14 +321,17 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
     for (int e = 0; e < kPer; ++e) {
       float cs, sn;
       const double freq = inv_freq.f[4 * kPer * i + kPer * g + e];
-      if (sizeof(T) == 2) rot_cos_sin_fast(pos, freq, &cs, &sn);          // (the result is rounded to bf16)
+      if (sizeof(T) == 2) rot_cos_sin_fast(pos, freq, &cs, &sn);          // (16 bits of the result are kept)
       else rot_cos_sin(pos, freq, &cs, &sn);
-      const float u = to_float(q[i][e]), w = to_float(q[i + kQ / 2][e]);
+      const float u = to_float(q[0][i][e]), w = to_float(q[0][i + kQ / 2][e]);
       x[e] = (u * cs - w * sn) * scale;
       y[e] = (w * cs + u * sn) * scale;
     }
-    q[i] = Keys::piece(x);
-    q[i + kQ / 2] = Keys::piece(y);
+#pragma unroll
+    for (int part = 0; part < Keys::kParts; ++part) {
+      q[part][i] = Keys::piece(x, part);
+      q[part][i + kQ / 2] = Keys::piece(y, part);
+    }
   }
 
   auto take = [&](Keys& t, const Page& held) __attribute__((always_inline)) {
@@ -364,9 +375,12 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
     for (int e = 0; e < kTok; ++e) { p[e] = __builtin_amdgcn_exp2f(s[e] - m); sum += p[e]; }
     l += sum;
     if (!apart) {
-      const Piece w = Keys::piece(p);
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) o[i] = Keys::add_values(t.v[i], w, o[i]);
+      for (int part = 0; part < Keys::kParts; ++part) {
+        const Piece w = Keys::piece(p, part);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) o[i] = Keys::add_values(t.v[i], w, o[i]);
+      }
     } else {
       // 0 x value would reach the columns that do not see it: one column at a time
 #pragma unroll 1
@@ -375,14 +389,18 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
         float only[kTok];
 #pragma unroll
         for (int e = 0; e < kTok; ++e) only[e] = n == k ? p[e] : 0.f;
-        const Piece w = Keys::piece(only);
+        Piece w[Keys::kParts];
+#pragma unroll
+        for (int part = 0; part < Keys::kParts; ++part) w[part] = Keys::piece(only, part);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
           Piece v = t.v[i];
 #pragma unroll
           for (int e = 0; e < kTok; ++e)
             if (e >= seen) v[e] = static_cast<T>(0.f);
-          const f32x4 add = Keys::add_values(v, w, f32x4{0.f, 0.f, 0.f, 0.f});
+          f32x4 add = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int part = 0; part < Keys::kParts; ++part) add = Keys::add_values(v, w[part], add);
           if (n == k) o[i] += add;
         }
       }
