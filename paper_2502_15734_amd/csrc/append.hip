@@ -13,11 +13,13 @@
 // dimension-major V row.  fp32, a tile of one page: steps of four tokens, as in qk_f32.hip.
 //
 // One pass: o = sum_t 2^(s_t - m) v_t and l = sum_t 2^(s_t - m), where the reference m of a column is shared by its lane groups and moves (o and l times
-// 2^(old - new)) only when a logit is more than kSlack above it.  m, l and o are fp32; queries, once they are turned to their position, and weights are rounded
-// to the element type, which is what the matrix instructions take.
+// 2^(old - new)) only when a logit is more than kSlack above it.  m, l and o are fp32.  Queries, once they are turned to their position, and weights are what
+// the matrix instructions take: bf16 as the sum of two up to 64 columns, where the bytes of the keys are the bound (one row over 700 tokens 12.3 -> 12.7 us, 32
+// requests 115.2 -> 115.6, 16 x 5 rows of 64 heads 79.6 -> 82.6; rms error against 64 bits 0.0029 -> 0.0017 of the output, which is its own rounding), as one
+// above, where the products are (their rounding, 2^-9 of a weight at most, is that of the attention of the prefill).
 //
 // 32 heads on 8 of 128, bf16: 32 requests of one row over 1500 to 6700 tokens 115 us (4.5 TB/s of keys and values; a copy of 4 GiB moves 4.7), one
-// row over 130 000 tokens 104 us (5.1 TB/s), one over 700 tokens 12.2 us, of which two launches take 5 and the chain of dependent loads (segments, page
+// row over 130 000 tokens 105 us (5.1 TB/s), one over 700 tokens 12.7 us, of which two launches take 5 and the chain of dependent loads (segments, page
 // table, page, parts) most of the rest.
 #include <algorithm>
 #include <type_traits>
@@ -151,6 +153,16 @@ __device__ __forceinline__ void write_rows(const AppendArgs& a, const InvFreq& i
   __syncthreads();                                     // (the workgroup's loads behind it see the rows)
 }
 
+// x as a bf16, or as the sum of two.  Part 0 of two: the upper 16 bits, x becomes the rest; the last part: the nearest bf16.  The rest keeps the sign and
+// is not 0, so that a product with an infinite factor is one infinity and not a difference of two.
+template <int PARTS>
+__device__ __forceinline__ bf16_t take_part(float& x, int part) {
+  if (part == PARTS - 1) return static_cast<bf16_t>(x);
+  const float up = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+  x = copysignf(fmaxf(fabsf(x - up), 0x1p-126f), up);
+  return static_cast<bf16_t>(up);
+}
+
 template <typename T, int D> struct Tile;           // operands of one tile of keys
 
 template <int D> struct Tile<bf16_t, D> {
@@ -187,16 +199,10 @@ template <int D> struct Tile<bf16_t, D> {
   static __device__ __forceinline__ f32x4 add_values(const Piece& v, const Piece& p, f32x4 o) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o, 0, 0, 0);
   }
-  // Part 0: the upper 16 bits, x becomes the rest; part 1: the nearest to that.  The rest keeps the sign and is not 0, so that a product with an infinite
-  // factor is one infinity and not a difference of two.
   static __device__ __forceinline__ Piece piece(float (&x)[8], int part) {
     Piece w;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float up = __uint_as_float(__float_as_uint(x[e]) & (part == 0 ? 0xffff0000u : 0xffffffffu));
-      w[e] = static_cast<bf16_t>(up);
-      x[e] = copysignf(fmaxf(fabsf(x[e] - up), 0x1p-126f), up);
-    }
+    for (int e = 0; e < 8; ++e) w[e] = take_part<2>(x[e], part);
     return w;
   }
 };
@@ -456,7 +462,7 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
 // A draft to check or a further question: 17 columns and more (rows times heads of a group) share the keys.  Workgroup = 32 CW columns x a range
 // of pages; tiles of 64 keys go through LDS (two images, loads that write LDS while the other is multiplied, one barrier per tile), so that a page is read
 // once for all its columns.  CW = 4: each wavefront multiplies its 32 columns with all 64 keys; CW = 2: two wavefronts per 32 columns take 32
-// keys each and meet at the end.  Few columns are bound by the bytes (16 requests of 5 rows over 1000 to 8000 tokens, 64 heads on 8: 78 us, 3.7 TB/s), from some
+// keys each and meet at the end.  Few columns are bound by the bytes (16 requests of 5 rows over 1000 to 8000 tokens, 64 heads on 8: 82 us, 3.6 TB/s), from some
 // hundred on by the vector instructions beside the matrix instructions: 500 rows of 32 heads over 16 000 tokens take 165 us, of them 150 in this
 // kernel, with the matrix cores busy for half of its cycles, LDS for a quarter, and the rest in what lies between two products of a tile (maximum, mask,
 // barrier) that the other workgroup of the compute unit does not cover.
@@ -580,7 +586,8 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
 
   // ---- the queries at their positions, in units of the logits' powers of two
   const float scale = rsqrtf(static_cast<float>(D)) * kLog2e;
-  bf16x8 q[D / 16];
+  constexpr int kParts = CW == 2 ? 2 : 1;                             // (see the head of the file)
+  bf16x8 q[kParts][D / 16];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
     const bf16x8 x = __builtin_bit_cast(bf16x8, raw[i]), y = __builtin_bit_cast(bf16x8, raw[i + D / 32]);
@@ -589,8 +596,12 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
       float cs, sn;
       rot_cos_sin_fast(pos, inv_freq.f[16 * i + 8 * h + e], &cs, &sn);
       const float u = to_float(x[e]), w = to_float(y[e]);
-      q[i][e] = static_cast<bf16_t>((u * cs - w * sn) * scale);
-      q[i + D / 32][e] = static_cast<bf16_t>((w * cs + u * sn) * scale);
+      float first = (u * cs - w * sn) * scale, second = (w * cs + u * sn) * scale;
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) {
+        q[part][i][e] = take_part<kParts>(first, part);
+        q[part][i + D / 32][e] = take_part<kParts>(second, part);
+      }
     }
   }
   f32x16 o[D / 32];
@@ -621,16 +632,27 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     auto key = [&](int b, int kk) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8*>(bytes + (k_at ^ (32 * kk)) + b * 64 * D); };
     auto value = [&](int b, int g, int j) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8*>(bytes + v_byte + (2 * b + g) * 32 * D + j * 512); };
     f32x16 s[kBlocks];
-    bf16x8 w[kBlocks][2];
+    bf16x8 w[kBlocks][2], rest[2];                                     // (rest: of the weights, with two parts)
     // the logits less the reference of the column, which enters as the products' first summand
     auto fence = []() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
+    auto first_summand = [&]() __attribute__((always_inline)) {          // (with two parts there are no registers to hold it)
+      if constexpr (kParts == 1) return from;
+      f32x16 x;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = -m;
+      return x;
+    };
     // weights of the two logits 2 x, 2 x + 1 of a block
     auto weigh = [&](int b, int x) __attribute__((always_inline)) {
-      const float x0 = __builtin_amdgcn_exp2f(s[b][2 * x]), x1 = __builtin_amdgcn_exp2f(s[b][2 * x + 1]);
+      float x0 = __builtin_amdgcn_exp2f(s[b][2 * x]), x1 = __builtin_amdgcn_exp2f(s[b][2 * x + 1]);
       l += x0;
       l += x1;
-      w[b][x / 4][2 * x % 8] = static_cast<bf16_t>(x0);
-      w[b][x / 4][2 * x % 8 + 1] = static_cast<bf16_t>(x1);
+      w[b][x / 4][2 * x % 8] = take_part<kParts>(x0, 0);
+      w[b][x / 4][2 * x % 8 + 1] = take_part<kParts>(x1, 0);
+      if constexpr (kParts == 2) {
+        rest[x / 4][2 * x % 8] = take_part<kParts>(x0, 1);
+        rest[x / 4][2 * x % 8 + 1] = take_part<kParts>(x1, 1);
+      }
     };
     // S(b); under it the weights of block `under` (-1: none)
     auto products = [&](int b, auto under) __attribute__((always_inline)) {
@@ -640,7 +662,8 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
       fence();
 #pragma unroll
       for (int kk = 0; kk < kSteps; ++kk) {
-        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kk % kAhead], q[kk], kk == 0 ? from : s[b], 0, 0, 0);
+        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kk % kAhead], q[0][kk], kk == 0 ? first_summand() : s[b], 0, 0, 0);
+        if constexpr (kParts == 2) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kk % kAhead], q[1][kk], s[b], 0, 0, 0);
         if (kk + kAhead < kSteps) k[kk % kAhead] = key(b, kk + kAhead);
         if constexpr (decltype(under)::value >= 0)
 #pragma unroll
@@ -704,6 +727,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
         for (int x = 0; x < kV; ++x) {
           const int j = x % (D / 32);
           o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[x % 4], w[b][x / (D / 32)], o[j], 0, 0, 0);
+          if constexpr (kParts == 2) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[x % 4], rest[x / (D / 32)], o[j], 0, 0, 0);
           if (x + 4 < kV) v[x % 4] = value(b, (x + 4) / (D / 32), (x + 4) % (D / 32));
           if constexpr (decltype(under)::value >= 0)
 #pragma unroll
@@ -720,6 +744,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = fabsf(to_float(v[e])) < INFINITY ? v[e] : static_cast<bf16_t>(0.f);
             o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[b][g], o[j], 0, 0, 0);
+            if constexpr (kParts == 2) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, rest[g], o[j], 0, 0, 0);
           }
           const int pg = (b0 + b) * 2 + g, first = list[i + pg].pos0;
           const bf16_t* values = reinterpret_cast<const bf16_t*>(img + 8 * D + pg * 2 * D);
@@ -729,7 +754,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
             asm volatile("" : "+v"(dim0));
             float weight = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) weight = t % 8 == e ? to_float(w[b][g][e]) : weight;
+            for (int e = 0; e < 8; ++e) weight = t % 8 == e ? to_float(w[b][g][e]) + (kParts == 2 ? to_float(rest[g][e]) : 0.f) : weight;
             weight = __shfl(weight, n + 32 * (t >> 3), 64);
             const bool sees = first + t <= pos;
 #pragma unroll
