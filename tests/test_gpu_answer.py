@@ -283,6 +283,55 @@ def test_append_attention_over_long_contexts(dtype, lengths, new):
     b.check(t)
 
 
+@pytest.mark.parametrize("hq,d,new", [(8, 128, 1), (8, 64, 4), (8, 128, 5), (12, 128, 10), (8, 64, 16)])
+def test_append_attention_few_columns_lose_nothing_inside(hq, d, new):
+    """Up to 64 rows and heads on a KV head, bf16: queries and weights are sums of two bf16, off by 2^-15 (2^-7 of the value is left to the second, which is
+    off by 2^-8 of that), not by 2^-8.  The angles' functions are off by 2e-6, so a logit by at most 4 e-6 max|q| sum|k| / sqrt d more.  Only the output's own
+    rounding is one of bf16."""
+    b = Batch(12, [((700, 33), 20, new), ((), 60, new), ((250,), 17, new)], hq, 2, d, "bf16")
+    t = b.up()
+    b.call(_ctx("bf16", hq, 2, d), t)
+    torch.cuda.synchronize()
+    k, v, out = t["k_pool"].float().cpu().numpy(), t["v_pool"].float().cpu().numpy(), t["out"].double().cpu().numpy()
+    for r in range(b.n_req):
+        rows = range(b.cu[r], b.cu[r + 1])
+        context = A.paged_context(k, v, lambda p: v[p], b.tab, b.segs, range(b.off[r], b.off[r + 1]))
+        q = b.q[rows].double().numpy()
+        o, _, bound, _ = A.attend(q, np.array(b.pos)[rows], *context, THETA, 2.0 ** -15)
+        turn = 4e-6 * np.abs(q).max() * np.abs(context[1]).sum(-1).max() / math.sqrt(d)
+        bound += 2.0 ** -8 * np.abs(o) + math.expm1(2 * turn) * np.abs(context[2]).max()
+        assert (np.abs(out[rows] - o) <= bound).all(), f"request {r}: {(np.abs(out[rows] - o) / bound).max():.3g} of the bound"
+
+
+@pytest.mark.parametrize("dtype,d,new", [("bf16", 128, 1), ("bf16", 64, 4), ("bf16", 128, 5), ("bf16", 64, 16), ("bf16", 128, 40), ("f32", 128, 3)])
+def test_append_attention_infinite_values_that_every_row_sees(dtype, d, new):
+    """An infinite value has a weight above 0 in every row: that dimension is infinite, the others are what they are without it.  One request has a
+    cached key with nine times the others' logits, above or below them."""
+    b = Batch(13, [((300,), 70, new), ((40,), 20 + new, new)], 8, 2, d, dtype)
+    b.k_pool[b.tab[b.segs[2][4]]][:, 5] *= 9
+    for s in (0, 2):
+        page = b.tab[b.segs[s][4] + 1]
+        b.v_pool[page, 0, 3, 4], b.v_pool[page, 0, 5, 9] = math.inf, -math.inf
+    t = b.up()
+    b.call(_ctx(dtype, 8, 2, d), t)
+    torch.cuda.synchronize()
+    out = t["out"].clone()
+    assert (out[:, :4, 3] == math.inf).all() and (out[:, :4, 5] == -math.inf).all()
+    finite = torch.isfinite(out)
+    finite[:, :4, [3, 5]] = True
+    assert finite.all()
+    plain = t["v_pool"].clone()
+    plain[torch.isinf(plain)] = 0.0
+    k, v, half = t["k_pool"].float().cpu().numpy(), plain.float().cpu().numpy(), 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    for r in range(2):
+        rows = range(b.cu[r], b.cu[r + 1])
+        o, _, bound, _ = A.attend(b.q[rows].double().numpy(), np.array(b.pos)[rows], *A.paged_context(k, v, lambda p: v[p], b.tab, b.segs, range(b.off[r], b.off[r + 1])),
+                                  THETA, half)
+        off = np.abs(out[rows].double().cpu().numpy() - o)
+        off[:, :4, [3, 5]] = 0
+        assert (off <= bound).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_append_attention_large_logits(dtype):
     """Logits of some hundred: the weights are those of one or two keys, and the running maximum moves."""
