@@ -623,7 +623,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   // steps are fenced, because the compiler by itself reads every operand right in front of its product and takes the exponentials together.
   auto compute = [&](auto set_aside, const u32x4* img, int i, int here, int flags) __attribute__((always_inline)) {
     constexpr bool ODD = decltype(set_aside)::value;
-    constexpr int kSteps = D / 16, kAhead = kSteps < 4 ? kSteps : 4;   // products of a block; operands in flight
+    constexpr int kSteps = D / 16, kAhead = 4;   // products of a block; operands in flight
     const int b0 = ks * kBlocks;                                       // this wavefront's first 32-key block
     // (the operands' addresses are made here again: kept over the loop they would cost a register each)
     const char* bytes = reinterpret_cast<const char*>(img);
@@ -631,6 +631,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     asm volatile("" : "+v"(k_at));
     auto key = [&](int b, int kk) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8*>(bytes + (k_at ^ (32 * kk)) + b * 64 * D); };
     auto value = [&](int b, int g, int j) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8*>(bytes + v_byte + (2 * b + g) * 32 * D + j * 512); };
+    bf16x8 ahead[kAhead];                                              // operands of the next products, also over the masks and maxima between two blocks
     f32x16 s[kBlocks];
     bf16x8 w[kBlocks][2], rest[2];                                     // (rest: of the weights, with two parts)
     // the logits less the reference of the column, which enters as the products' first summand
@@ -656,15 +657,17 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     };
     // S(b); under it the weights of block `under` (-1: none)
     auto products = [&](int b, auto under) __attribute__((always_inline)) {
-      bf16x8 k[kAhead];
+      if (ODD || b == 0)
 #pragma unroll
-      for (int kk = 0; kk < kAhead; ++kk) k[kk] = key(b, kk);
+        for (int kk = 0; kk < kAhead; ++kk) ahead[kk] = key(b, kk);
       fence();
 #pragma unroll
       for (int kk = 0; kk < kSteps; ++kk) {
-        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kk % kAhead], q[0][kk], kk == 0 ? first_summand() : s[b], 0, 0, 0);
-        if constexpr (kParts == 2) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kk % kAhead], q[1][kk], s[b], 0, 0, 0);
-        if (kk + kAhead < kSteps) k[kk % kAhead] = key(b, kk + kAhead);
+        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[kk % kAhead], q[0][kk], kk == 0 ? first_summand() : s[b], 0, 0, 0);
+        if constexpr (kParts == 2) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[kk % kAhead], q[1][kk], s[b], 0, 0, 0);
+        if (kk + kAhead < kSteps) ahead[kk % kAhead] = key(b, kk + kAhead);
+        else if (!ODD && b + 1 < kBlocks) ahead[kk % kAhead] = key(b + 1, kk + kAhead - kSteps);
+        else if (!ODD) ahead[kk % kAhead] = value(0, (kk + kAhead - kSteps) / (D / 32), (kk + kAhead - kSteps) % (D / 32));
         if constexpr (decltype(under)::value >= 0)
 #pragma unroll
           for (int x = 0; x < 8 / kSteps; ++x) weigh(decltype(under)::value, kk * (8 / kSteps) + x);
@@ -718,17 +721,15 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     // o += V P(b); under it the weights of block `under`
     auto add_values = [&](int b, auto under) __attribute__((always_inline)) {
       if constexpr (!ODD) {
-        bf16x8 v[4];
         constexpr int kV = D / 16;                                     // products: two pages of D / 32 groups of dims
-#pragma unroll
-        for (int x = 0; x < 4; ++x) v[x] = value(b, x / (D / 32), x % (D / 32));
         fence();
 #pragma unroll
         for (int x = 0; x < kV; ++x) {
           const int j = x % (D / 32);
-          o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[x % 4], w[b][x / (D / 32)], o[j], 0, 0, 0);
-          if constexpr (kParts == 2) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[x % 4], rest[x / (D / 32)], o[j], 0, 0, 0);
-          if (x + 4 < kV) v[x % 4] = value(b, (x + 4) / (D / 32), (x + 4) % (D / 32));
+          o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[x % 4], w[b][x / (D / 32)], o[j], 0, 0, 0);
+          if constexpr (kParts == 2) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[x % 4], rest[x / (D / 32)], o[j], 0, 0, 0);
+          if (x + 4 < kV) ahead[x % 4] = value(b, (x + 4) / (D / 32), (x + 4) % (D / 32));
+          else if (b + 1 < kBlocks) ahead[x % 4] = value(b + 1, (x + 4 - kV) / (D / 32), (x + 4 - kV) % (D / 32));
           if constexpr (decltype(under)::value >= 0)
 #pragma unroll
             for (int y = 0; y < 8 / kV; ++y) weigh(decltype(under)::value, x * (8 / kV) + y);
