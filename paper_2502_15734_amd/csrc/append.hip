@@ -774,13 +774,16 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     constexpr std::integral_constant<int, -1> none;
     constexpr std::integral_constant<int, 0> first_block;
     constexpr std::integral_constant<int, 1> second_block;
-    __builtin_amdgcn_s_setprio(1);                                     // (2 %: a wavefront that stages or waits stands back)
     products(0, none);
     settle(0, 0);
     if constexpr (kBlocks == 2 && !ODD) {
+      // (ahead of the compute unit's other workgroup while exponentials and products go together, behind it where there are products alone: 500 rows
+      // over 16 000 tokens 160.8 -> 157, with the whole tile ahead; 165 without)
+      __builtin_amdgcn_s_setprio(1);
       products(1, first_block);
       settle(1, 1);
       add_values(0, second_block);
+      __builtin_amdgcn_s_setprio(0);
       add_values(1, none);
     } else {
 #pragma unroll
@@ -794,7 +797,6 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
         add_values(1, none);
       }
     }
-    __builtin_amdgcn_s_setprio(0);
   };
 
   // ---- the keys, until no column of the workgroup sees them
