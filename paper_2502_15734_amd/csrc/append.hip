@@ -463,8 +463,8 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
 // of pages; tiles of 64 keys go through LDS (two images, loads that write LDS while the other is multiplied, one barrier per tile), so that a page is read
 // once for all its columns.  CW = 4: each wavefront multiplies its 32 columns with all 64 keys; CW = 2: two wavefronts per 32 columns take 32
 // keys each and meet at the end.  Few columns are bound by the bytes (16 requests of 5 rows over 1000 to 8000 tokens, 64 heads on 8: 82 us, 3.6 TB/s), from some
-// hundred on by the vector instructions beside the matrix instructions: 500 rows of 32 heads over 16 000 tokens take 165 us, of them 150 in this
-// kernel, with the matrix cores busy for half of its cycles, LDS for a quarter, and the rest in what lies between two products of a tile (maximum, mask,
+// hundred on by the vector instructions beside the matrix instructions: 500 rows of 32 heads over 16 000 tokens take 158 us, of them 140 to 150 in
+// this kernel, with the matrix cores busy for 54 % of its cycles, LDS for 30, and the rest in what lies between two products of a tile (maximum, mask,
 // barrier) that the other workgroup of the compute unit does not cover.
 //
 // v_mfma_f32_32x32x16_bf16, S^T = K Q^T and O^T = V^T P^T with lane = (n = lane % 32, h = lane / 32), column n.  As above the key rows are

@@ -18,7 +18,7 @@
 //
 // Few rows are bound by latency: four launches, each with a chain of two or three loads, scans and barriers (1 x 32000 fp32 with top-p 23.6 us, of
 // which the last kernel takes 8; 32 x 128256 bf16 36 us).  Many rows are bound by the three reads and the arithmetic in 64 bits beside the second and third:
-// 256 x 128001 fp32 (131 MB) with all kinds of settings 106 us: 26 for the first pass (5 TB/s), 26, 36 and 13 to 25 for the last kernel, the
+// 256 x 128001 fp32 (131 MB) with all kinds of settings 104 us: 26 for the first pass (5 TB/s), 26, 36 and 11 to 24 for the last kernel, the
 // longest where a row has many candidates to sort.
 #include <algorithm>
 
