@@ -14,7 +14,8 @@
 //                        logits of that bin, the candidates
 //   sample_draw_kernel   sorts the candidates, finds the cut among them, the tile the drawn number falls into and the token in it
 // Rows with more candidates than the list holds (thousands of equal logits) are done by the last kernel alone, with radix descents
-// over the whole row (32000 equal ones 0.6 ms, 128256 2 ms); vocabularies that fit the list need no other kernel than the last.
+// over the whole row (32000 equal ones 0.6 ms, 128256 2 ms).  Rows of up to 12 Ki logits are the last kernel's alone: it holds them in LDS and takes the
+// same steps there.
 //
 // Few rows are bound by latency: four launches, each with a chain of two or three loads, scans and barriers (1 x 32000 fp32 with top-p 23.6 us, of
 // which the last kernel takes 8; 32 x 128256 bf16 36 us).  Many rows are bound by the three reads and the arithmetic in 64 bits beside the second and third:
@@ -296,7 +297,7 @@ struct Weights {
 constexpr int kBins = 1024, kMaxParts = 64, kList = 4096, kLocal = 512;     // (kLocal: candidates of a part that are gathered in LDS)
 
 struct SamplePlan {
-  int parts, part_len;                // a part is read by a workgroup, a quarter of it by a wavefront; parts 0: the list holds a row
+  int parts, part_len;                // a part is read by a workgroup, a quarter of it by a wavefront; parts 0: the last kernel alone
   int wave_tiles, tile_len;           // a wavefront's quarter has 1, 2 or 4 tiles, whose sums are kept
 };
 constexpr int kTiles = 256;           // of a row
@@ -403,7 +404,7 @@ struct Bins {
 // Where the cuts fall, from the histogram.  With both top-k and top-p the weight that top-p refers to is known to the bin that top-k's cut
 // falls into, so top-p's has a first and a last possible bin.
 template <int N>
-__device__ __forceinline__ Cuts find_cuts(const RowScratch& ws, const RowSettings& s, bool far) {
+__device__ __forceinline__ Cuts find_cuts(const unsigned* counts, const unsigned long long* masses, const RowSettings& s, bool far) {
   constexpr int kOwn = kBins / N;     // bins of a thread
   __shared__ unsigned long long wave_mass[N / 64];
   __shared__ unsigned wave_count[N / 64];
@@ -413,8 +414,8 @@ __device__ __forceinline__ Cuts find_cuts(const RowScratch& ws, const RowSetting
   unsigned long long m[kOwn], mass = 0;
 #pragma unroll
   for (int i = 0; i < kOwn; ++i) {
-    c[i] = ws.count[tid * kOwn + i];
-    m[i] = ws.mass[tid * kOwn + i];
+    c[i] = counts[tid * kOwn + i];
+    m[i] = masses[tid * kOwn + i];
     count += c[i];
     mass += m[i];
   }
@@ -555,6 +556,35 @@ __global__ __launch_bounds__(256) void sample_hist_kernel(SampleArgs a, SamplePl
     }
 }
 
+// What becomes of a logit once the cuts are known.
+struct Sieve {
+  const Weights& weights;
+  const Bins& bins;
+  bool cut;
+  int p_lo, p_hi, k_bin;
+  float least_z, floor;               // logits below least_z are below min-p for certain, and those below floor are neither kept nor candidates: 2^-20 and a bin for the roundings
+  __device__ __forceinline__ Sieve(const RowSettings& s, const Weights& w, const Bins& b, const Cuts& c, bool cut_) : weights(w), bins(b), cut(cut_) {
+    p_lo = cut ? c.p_lo : kBins;
+    p_hi = cut ? c.p_hi : kBins;
+    k_bin = cut ? c.k_bin : kBins;
+    const double reach = log(s.min_p) / s.inv_t;         // (-inf without min-p; a NaN: no such logit)
+    least_z = static_cast<float>(w.top + reach - 0x1p-20 * (fabs(w.top) - reach));
+    const int last_bin = k_bin < kBins ? max(p_hi, k_bin) : p_hi;
+    floor = !cut ? least_z : last_bin < kBins - 2 ? b.top - (last_bin + 2) / b.per : -INFINITY;
+  }
+  template <typename F>
+  __device__ __forceinline__ void take(float z, unsigned& kept, unsigned long long& sum, F&& candidate) const {
+    const int b = cut ? bins.of(z) : -1;
+    if (b < p_lo) {
+      if (z < least_z) return;
+      const double w = weights.scaled(z);
+      if (w >= weights.least) { ++kept; sum += Weights::whole(w); }
+    } else if (b <= p_hi || b == k_bin) {
+      candidate();
+    }
+  }
+};
+
 template <typename T>
 __global__ __launch_bounds__(256) void sample_tiles_kernel(SampleArgs a, SamplePlan plan, RowScratch* __restrict__ scratch) {
   constexpr int kPer = RowReader<T>::kPer;
@@ -572,33 +602,23 @@ __global__ __launch_bounds__(256) void sample_tiles_kernel(SampleArgs a, SampleP
   if (!(fabsf(x.top) < INFINITY) || (cut && !bins.usable)) return;
   const Weights weights(x.top, s, a.shift, table);
   __syncthreads();
-  int p_lo = kBins, p_hi = kBins, k_bin = kBins;
+  Cuts c{};
   if (cut) {
-    const Cuts c = find_cuts<256>(ws, s, bins.far);
+    c = find_cuts<256>(ws.count, ws.mass, s, bins.far);
     if (part == 0 && tid == 0) ws.cuts = c;
     if (c.listed > kList) return;                      // (the last kernel does the row alone)
-    p_lo = c.p_lo; p_hi = c.p_hi; k_bin = c.k_bin;
   }
+  const Sieve sieve(s, weights, bins, c, cut);
   const RowReader<T> in(a, row);
   const int tile0 = (part * 4 + wave) * plan.wave_tiles;
-  // (logits below least_z are below min-p for certain, and those below floor are neither kept nor candidates: 2^-20 and a bin for the roundings)
-  const double reach = log(s.min_p) / s.inv_t;         // (-inf without min-p; a NaN: no such logit)
-  const float least_z = static_cast<float>(weights.top + reach - 0x1p-20 * (fabs(weights.top) - reach));
-  const int last_bin = k_bin < kBins ? max(p_hi, k_bin) : p_hi;
-  const float floor = !cut ? least_z : last_bin < kBins - 2 ? x.top - (last_bin + 2) / bins.per : -INFINITY;
   unsigned kept[4] = {0, 0, 0, 0};
   unsigned long long sum[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int t = 0; t < 4; ++t)
     if (t < plan.wave_tiles) {
       const int e0 = (tile0 + t) * plan.tile_len;
-      in.each(e0 + lane * kPer, min(e0 + plan.tile_len, a.vocab + in.shift), 64 * kPer, floor, [&](float z, int i) __attribute__((always_inline)) {
-        const int b = cut ? bins.of(z) : -1;
-        if (b < p_lo) {
-          if (z < least_z) return;
-          const double w = weights.scaled(z);
-          if (w >= weights.least) { ++kept[t]; sum[t] += Weights::whole(w); }
-        } else if (b <= p_hi || b == k_bin) {
+      in.each(e0 + lane * kPer, min(e0 + plan.tile_len, a.vocab + in.shift), 64 * kPer, sieve.floor, [&](float z, int i) __attribute__((always_inline)) {
+        sieve.take(z, kept[t], sum[t], [&]() __attribute__((always_inline)) {
           const unsigned at = atomicAdd(&n_list, 1u);
           if (at < kLocal) {
             list[at] = make_uint2(logit_key(z), i);
@@ -606,7 +626,7 @@ __global__ __launch_bounds__(256) void sample_tiles_kernel(SampleArgs a, SampleP
             const unsigned to = atomicAdd(&ws.n_list, 1u);
             if (to < kList) ws.list[to] = make_uint2(logit_key(z), i);
           }
-        }
+        });
       });
     }
 #pragma unroll
@@ -703,118 +723,179 @@ __device__ __forceinline__ void sort_down(unsigned long long* order, int n_pow) 
   __syncthreads();
 }
 
-// W wavefronts.
-template <typename T, int W>
+// W wavefronts.  ROW: bytes of LDS that hold the row, of which this is then the only kernel; 0: it comes behind the others.
+template <typename T, int W, int ROW>
 __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, SamplePlan plan, RowScratch* __restrict__ scratch) {
+  constexpr bool kParts = ROW == 0;
+  constexpr int kThreads = 64 * W, kCap = kParts ? kList : 1024, kPer = RowReader<T>::kPer, kBinsHere = kParts ? 1 : kBins;
+  typedef typename RowReader<T>::Piece Piece;
   union Shared {
     RowShared<W> row;
-    struct { unsigned long long order[kList]; unsigned long long tile[kTiles]; } list;
+    struct { unsigned long long mass[kBinsHere]; unsigned count[kBinsHere]; } bins;
+    struct { unsigned long long order[kCap]; unsigned long long tile[kTiles]; } list;
   };
   __shared__ Shared sh;
-  constexpr int kThreads = 64 * W;
+  __shared__ Piece held[kParts ? 1 : ROW / 16];
   __shared__ unsigned long long part_mass[W], found_before;
-  __shared__ unsigned part_count[W];
+  __shared__ unsigned part_count[W], n_found;
+  __shared__ Part wave_part[W];
   __shared__ int found;
   __shared__ double table[kTable];
-  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const RowSettings s = settings_of(a, row);
-  const bool parts = plan.parts > 0, cut = !parts || needs_cut(a, s);
+  const bool cut = needs_cut(a, s);
   const RowReader<T> in(a, row);
-  const int tile_len = parts ? plan.tile_len : kList, shift = parts ? in.shift : 0, n_tiles = parts ? 4 * plan.wave_tiles * plan.parts : 1;
-  uint32_t top;
-  int top_idx;
-  Part x{0, 0, 0, 0};
+  const int shift = in.shift, n_pieces = (a.vocab + shift + kPer - 1) / kPer, tile_pieces = (n_pieces + 4 * W - 1) / (4 * W);
+  const int tile_len = kParts ? plan.tile_len : tile_pieces * kPer, n_tiles = kParts ? 4 * plan.wave_tiles * plan.parts : 4 * W;
+  Part x{-INFINITY, INFINITY, 0x7fffffff, 0};
   Cuts c{};
   int n_list = 0;
-  bool whole = false;                                  // the list does not hold the candidates
   // (what the other kernels left, in one trip to memory; what this row does not use is not looked at)
   uint2 listed{0, 0};
   unsigned long long tile_mass = 0;
   unsigned tile_kept = 0;
-  if (parts) {
+  if constexpr (kParts) {
     const RowScratch& ws = scratch[row];
     c = ws.cuts;
     listed = ws.list[tid];
     if (tid < n_tiles) { tile_mass = ws.tile_mass[tid]; tile_kept = ws.tile_kept[tid]; }
     x = row_extremes(ws, plan.parts);
-    top = logit_key(x.top);
-    top_idx = x.top_idx;
   } else {
-    // the whole row is the list: (key, ~index), nothing behind it
-    unsigned mine = 0;
-    for (int i = tid; i < a.vocab; i += kThreads) {
-      const uint32_t k = key_at<T>(a, row, i);
-      sh.list.order[i] = k > kKeyNone ? (static_cast<unsigned long long>(k) << 32) | ~static_cast<uint32_t>(i) : 0ull;
-      mine += k > kKeyNone;
+    constexpr int kAhead = 4;
+    for (int b = tid; b < kBins; b += kThreads) { sh.bins.count[b] = 0; sh.bins.mass[b] = 0; }
+    if (tid == 0) n_found = 0;
+    for (int p0 = tid; p0 < n_pieces; p0 += kAhead * kThreads) {
+      Piece v[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = (p0 + j * kThreads) * kPer - shift;
+        if (i >= 0 && i + kPer <= a.vocab) v[j] = *reinterpret_cast<const Piece*>(in.row + i);
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int p = p0 + j * kThreads, i = p * kPer - shift;
+        if (p >= n_pieces) break;
+        const bool inside = i >= 0 && i + kPer <= a.vocab;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+          if (!inside) v[j][e] = i + e >= 0 && i + e < a.vocab ? in.row[i + e] : static_cast<T>(-INFINITY);
+          const float z = to_float(v[j][e]);
+          if (z > x.top) { x.top = z; x.top_idx = i + e; }
+          if (z > -INFINITY) x.low = fminf(x.low, z);
+        }
+        held[p] = v[j];
+      }
     }
-    n_list = a.vocab;
-    const unsigned finite = block_sum<W>(mine, part_count);
-    c.count_hi = finite;
-    uint32_t hi = 0;
-    int at = 0x7fffffff;
-    for (int i = tid; i < a.vocab; i += kThreads) {
-      const uint32_t k = static_cast<uint32_t>(sh.list.order[i] >> 32);
-      if (k > hi) { hi = k; at = i; }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const float t = __shfl_xor(x.top, o, 64);
+      const int i = __shfl_xor(x.top_idx, o, 64);
+      if (ahead(t, i, x.top, x.top_idx)) { x.top = t; x.top_idx = i; }
+      x.low = fminf(x.low, __shfl_xor(x.low, o, 64));
     }
-    unsigned long long best = hi == 0 ? 0ull : (static_cast<unsigned long long>(hi) << 32) | ~static_cast<uint32_t>(at);
-    for (int o = 32; o > 0; o >>= 1) best = max(best, __shfl_xor(best, o, 64));
+    if (lane == 0) wave_part[wave] = x;
     __syncthreads();
-    if (lane == 0) part_mass[tid >> 6] = best;
-    __syncthreads();
-    for (int w = 0; w < W; ++w) best = max(best, part_mass[w]);
-    top = static_cast<uint32_t>(best >> 32);
-    top_idx = static_cast<int>(~static_cast<uint32_t>(best));
-    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const Part o = wave_part[w];
+      if (ahead(o.top, o.top_idx, x.top, x.top_idx)) { x.top = o.top; x.top_idx = o.top_idx; }
+      x.low = fminf(x.low, o.low);
+    }
   }
+  const uint32_t top = logit_key(x.top);
   if (top <= kKeyNone || s.greedy) {                   // (nothing to draw; or nothing else than the largest)
     if (tid == 0) {
       const bool none = top <= kKeyNone;
-      a.token[row] = none ? -1 : top_idx;
+      a.token[row] = none ? -1 : x.top_idx;
       if (a.logprob != nullptr) a.logprob[row] = none ? -INFINITY : 0.f;
       if (a.n_kept != nullptr) a.n_kept[row] = none ? 0 : 1;
     }
     return;
   }
-  const float top_logit = logit_of(top);
-  const Bins bins(top_logit, parts ? x.low : top_logit, s.inv_t);
-  whole = top == kKeyInf || (parts && cut && !bins.usable);
-  const Weights weights(top_logit, s, a.shift, table);
+  const Bins bins(x.top, x.low, s.inv_t);
+  bool whole = top == kKeyInf || (cut && !bins.usable);        // the list does not hold the candidates
+  const Weights weights(x.top, s, a.shift, table);
   __syncthreads();
-  if (!whole && parts && cut) {
-    whole = c.listed > kList;
-    n_list = static_cast<int>(c.listed);
-    if (!whole)
-      for (int i = tid; i < n_list; i += kThreads) {
-        const uint2 v = i == tid ? listed : scratch[row].list[i];
-        sh.list.order[i] = (static_cast<unsigned long long>(v.x) << 32) | ~v.y;
+  if constexpr (!kParts)
+    if (!whole && cut) {
+      const bool weigh = s.top_p < 1.0;
+      for (int p = tid; p < n_pieces; p += kThreads) {
+        const Piece v = held[p];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+          const float z = to_float(v[e]);
+          if (!(z > -INFINITY)) continue;
+          const int b = bins.of(z);
+          atomicAdd(&sh.bins.count[b], 1u);
+          if (weigh) atomicAdd(&sh.bins.mass[b], Weights::whole(weights.scaled(z)));
+        }
       }
+      __syncthreads();
+      c = find_cuts<kThreads>(sh.bins.count, sh.bins.mass, s, bins.far);
+    }
+  if (!whole && cut) {
+    whole = c.listed > kCap;
+    n_list = static_cast<int>(c.listed);
   }
   if (whole) {
+    __syncthreads();
     sample_row<T, W>(a, row, s, top, sh.row);
     return;
+  }
+  if constexpr (kParts) {
+    for (int i = tid; i < n_list; i += kThreads) {
+      const uint2 v = i == tid ? listed : scratch[row].list[i];
+      sh.list.order[i] = (static_cast<unsigned long long>(v.x) << 32) | ~v.y;
+    }
+    if (tid < n_tiles) sh.list.tile[tid] = tile_mass;   // (n_tiles is at most the number of threads)
+  } else {
+    const Sieve sieve(s, weights, bins, c, cut);
+    __syncthreads();                                   // (the bins' place is the list's)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int tile = wave * 4 + t, q1 = min((tile + 1) * tile_pieces, n_pieces);
+      unsigned kept = 0;
+      unsigned long long sum = 0;
+      for (int p = tile * tile_pieces + lane; p < q1; p += 64) {
+        const Piece v = held[p];
+        float most = to_float(v[0]);
+#pragma unroll
+        for (int e = 1; e < kPer; ++e) most = fmaxf(most, to_float(v[e]));
+        if (most < sieve.floor) continue;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+          const float z = to_float(v[e]);
+          if (z > -INFINITY)
+            sieve.take(z, kept, sum, [&]() __attribute__((always_inline)) {
+              sh.list.order[atomicAdd(&n_found, 1u)] = (static_cast<unsigned long long>(logit_key(z)) << 32) | ~static_cast<uint32_t>(p * kPer + e - shift);
+            });
+        }
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) { kept += __shfl_xor(kept, o, 64); sum += __shfl_xor(sum, o, 64); }
+      if (lane == 0) { sh.list.tile[tile] = sum; tile_kept += kept; }
+    }
   }
   // ---- the candidates in order
   int n_pow = 1;
   while (n_pow < n_list) n_pow <<= 1;
   for (int i = n_list + tid; i < n_pow; i += kThreads) sh.list.order[i] = 0ull;
-  if (tid < n_tiles) sh.list.tile[tid] = tile_mass;   // (n_tiles is at most the number of threads)
   __syncthreads();
   if (n_pow <= kThreads) sort_down<1, kThreads>(sh.list.order, n_pow);
-  else if (n_pow == 2 * kThreads) sort_down<2, kThreads>(sh.list.order, n_pow);
-  else if (n_pow == 4 * kThreads) sort_down<4, kThreads>(sh.list.order, n_pow);
-  else if constexpr (kList > 4 * kThreads) {
-    if (n_pow == 8 * kThreads) sort_down<8, kThreads>(sh.list.order, n_pow);
+  else if constexpr (kCap > kThreads) {
+    if (n_pow == 2 * kThreads) sort_down<2, kThreads>(sh.list.order, n_pow);
+    else if (n_pow == 4 * kThreads) sort_down<4, kThreads>(sh.list.order, n_pow);
+    else if (n_pow == 8 * kThreads) sort_down<8, kThreads>(sh.list.order, n_pow);
     else sort_down<16, kThreads>(sh.list.order, n_pow);
   }
   // ---- the cut among them.  This thread's are own .. own + per
   const int per = max(1, n_pow / kThreads), own = tid * per;
   auto weight_at = [&](int i) { return weights.scaled(logit_of(static_cast<uint32_t>(sh.list.order[i] >> 32))); };
   int n_cand = n_list, kept_list = 0;
-  if (!parts) n_cand = static_cast<int>(c.count_hi);
   if (cut) {
-    const bool by_k = parts ? c.k_bin < kBins : s.top_k < n_cand;
+    const bool by_k = c.k_bin < kBins;
     // tokens that pass top-k: the list's first n_k.  (Candidates of p_lo .. p_hi come first; k_bin is among or behind them.)
-    const int base_k = !parts ? 0 : c.k_bin <= c.p_hi ? static_cast<int>(c.count_k - c.count_lo) : static_cast<int>(c.count_hi - c.count_lo);
+    const int base_k = c.k_bin <= c.p_hi ? static_cast<int>(c.count_k - c.count_lo) : static_cast<int>(c.count_hi - c.count_lo);
     const int n_k = by_k ? base_k + s.top_k - static_cast<int>(c.count_k) : n_cand;
     unsigned long long in_k = 0, mine = 0;
     for (int i = own; i < min(own + per, n_cand); ++i) {
@@ -825,7 +906,7 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
     unsigned long long mass_k = 0;
     if (s.top_p < 1.0) {
       mass_k = block_sum<W>(in_k, part_mass);
-      mass_k = parts && !by_k ? c.mass_all : c.mass_k + mass_k;
+      mass_k = !by_k ? c.mass_all : c.mass_k + mass_k;
     }
     unsigned long long before = c.mass_lo + block_before<W>(mine, part_mass);
     const double target = s.top_p * static_cast<double>(mass_k);
@@ -848,7 +929,7 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
   // ---- the tile the number falls into
   const unsigned long long here = tid < n_tiles ? sh.list.tile[tid] : 0ull;
   const unsigned long long front = block_before<W>(here, part_mass), total = block_sum<W>(here, part_mass);
-  const unsigned n_kept = block_sum<W>(tile_kept, part_count) + kept_list + (parts && cut ? c.unlisted : 0u);
+  const unsigned n_kept = block_sum<W>(tile_kept, part_count) + kept_list + (cut ? c.unlisted : 0u);
   const double target = s.u * static_cast<double>(total);
   if (static_cast<double>(front) <= target && static_cast<double>(front + here) > target) { found = tid; found_before = front; }
   __syncthreads();
@@ -856,9 +937,9 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
   auto kept_weight = [&](int e) {
     const int i = e - shift;
     if (i < 0) return 0.0;
-    const float z = to_float(in.row[i]);
+    const float z = to_float(kParts ? in.row[i] : reinterpret_cast<const T*>(held)[e]);
     if (!(z > -INFINITY)) return 0.0;
-    if (cut && !(parts && bins.of(z) < c.p_lo) && ((static_cast<unsigned long long>(logit_key(z)) << 32) | ~static_cast<uint32_t>(i)) < last) return 0.0;
+    if (cut && bins.of(z) >= c.p_lo && ((static_cast<unsigned long long>(logit_key(z)) << 32) | ~static_cast<uint32_t>(i)) < last) return 0.0;
     const double w = weights.scaled(z);
     return w >= weights.least ? w : 0.0;
   };
@@ -878,12 +959,17 @@ __global__ __launch_bounds__(64 * W) void sample_draw_kernel(SampleArgs a, Sampl
     }
 }
 
+// Rows of up to 12 Ki logits are one kernel's, which holds them in LDS (smaller ones in less of it, so that several workgroups share a compute unit).  1, 32 and 256 rows
+// of 5000 fp32 logits 14.7, 24.7 and 27.2 us, in parts 17.0, 26.4 and 31.6; of 16000 16.3, 28.7 and 32.8, in parts 16.8, 26.1 and 39.2; one row of 32000
+// 29.4 and 23.8 (a compute unit alone takes 5 us for the weights of so many).
+constexpr int kSmallRow = 16384, kLargeRow = 49152, kRowLogits = (kLargeRow - 32) / 4;     // bytes of LDS, of which 32 are for a row's beginning and end inside pieces
+
 // Parts of 2048 to 8192 logits, so many that a call has about a thousand workgroups (four on a compute unit), at most 64 a row.  32 x 128256 with 1024
 // workgroups 36 us, with 512 or 2048 43; 256 x 128001 in parts of 8192 113 us, of 4096 or 16384 126 (rows differ in work: shorter parts even it
 // out, and each part has its cuts to find).  Workgroups of 16 wavefronts took longer throughout (1 x 32000 27.7 us instead of 23.5, 64 x 128256 57 instead of 49).
 SamplePlan sample_plan(int n_rows, int vocab) {
   SamplePlan p{0, 0, 0, 0};
-  if (vocab <= kList) return p;
+  if (vocab <= kRowLogits) return p;
   const long long wanted = std::max(1, std::min(kMaxParts, 1024 / std::max(1, n_rows)));
   const long long most = (vocab + 8 + kMaxParts - 1) / kMaxParts;                  // (8: a row's beginning inside a piece)
   const long long len = std::max(most, std::min<long long>(std::max((vocab + 8 + wanted - 1) / wanted, 2048ll), 8192));
@@ -908,8 +994,9 @@ static void launch_sample_t(const SampleArgs& a, const SamplePlan& plan, RowScra
     hipLaunchKernelGGL(sample_tiles_kernel<T>, grid, dim3(256), 0, stream, a, plan, ws);
   }
   // (behind other kernels a workgroup of four wavefronts: its barriers and sums over wavefronts are most of its time, and four of them have fewer)
-  if (plan.parts > 0) hipLaunchKernelGGL((sample_draw_kernel<T, 4>), dim3(a.n_rows), dim3(256), 0, stream, a, plan, ws);
-  else hipLaunchKernelGGL((sample_draw_kernel<T, 16>), dim3(a.n_rows), dim3(1024), 0, stream, a, plan, ws);
+  if (plan.parts > 0) hipLaunchKernelGGL((sample_draw_kernel<T, 4, 0>), dim3(a.n_rows), dim3(256), 0, stream, a, plan, ws);
+  else if (a.vocab * sizeof(T) + 32 <= kSmallRow) hipLaunchKernelGGL((sample_draw_kernel<T, 16, kSmallRow>), dim3(a.n_rows), dim3(1024), 0, stream, a, plan, ws);
+  else hipLaunchKernelGGL((sample_draw_kernel<T, 16, kLargeRow>), dim3(a.n_rows), dim3(1024), 0, stream, a, plan, ws);
 }
 
 void launch_sample(const void* logits, int logits_dtype, int n_rows, int vocab, long long stride, const float* temperature,

@@ -509,6 +509,18 @@ def test_sample(rows, vocab, pad, dtype, settings):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab,pad", [(1023, 1), (4088, 3), (4089, 0), (8176, 5), (8177, 1), (12280, 7), (12281, 1)])
+def test_sample_where_rows_stop_fitting(vocab, pad, dtype):
+    """Vocabularies on both sides of what is held at once, rows that begin inside a piece of 16 bytes."""
+    rng = np.random.default_rng(vocab)
+    z = _logits(vocab, 9, vocab, dtype, pad)
+    for s in (dict(top_k=rng.integers(1, 80, 9)), dict(top_p=rng.uniform(0.3, 0.99, 9), temperature=rng.uniform(0.4, 1.4, 9)),
+              dict(top_k=rng.integers(2, 900, 9), top_p=rng.uniform(0.3, 0.99, 9), min_p=rng.uniform(0.0, 0.02, 9)), dict(min_p=rng.uniform(0.0, 0.2, 9)), {}):
+        u = rng.random(9, dtype=np.float32)
+        _check_sample(_sample(_ctx(), z, vocab, u, **s), z, vocab, u, **s)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("vocab", [70, 5000, 40000])
 def test_sample_ties(vocab, dtype):
     """Rows of few distinct logits: cuts fall among equals, and the lowest indexes stay."""
