@@ -146,8 +146,13 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const R
       for (int i = tid; i < n; i += 64 * W) {
         const uint32_t k = key_at<T>(a, row, i);
         if (k <= kKeyNone || (digit < 3 && (k >> (8 * digit + 8)) != prefix)) continue;
-        atomicAdd(&count[(k >> (8 * digit)) & 255], 1u);
-        atomicAdd(&mass[(k >> (8 * digit)) & 255], fixed_of(weight_of(k, top, s.inv_t), a.shift));
+        // (lanes with one logit add it together: such rows are why this is called, and 64 sums of one place would follow each other)
+        const unsigned long long here = __ballot(true);
+        const bool one = __ballot(k == static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(k)))) == here;
+        if (one && lane != __builtin_ctzll(here)) continue;
+        const unsigned n_same = one ? __popcll(here) : 1u;
+        atomicAdd(&count[(k >> (8 * digit)) & 255], n_same);
+        atomicAdd(&mass[(k >> (8 * digit)) & 255], n_same * fixed_of(weight_of(k, top, s.inv_t), a.shift));
       }
       __syncthreads();
       if (tid == 0) {
