@@ -14,7 +14,7 @@
 //                        logits of that bin, the candidates
 //   sample_draw_kernel   sorts the candidates, finds the cut among them, the tile the drawn number falls into and the token in it
 // Rows with more candidates than the list holds (thousands of equal logits) are done by the last kernel alone, with radix descents
-// over the whole row (32000 equal ones 0.6 ms, 128256 2 ms).  Rows of up to 12 Ki logits are the last kernel's alone: it holds them in LDS and takes the
+// over the whole row (32000 equal ones 0.4 ms, 128256 1.25 ms).  Rows of up to 12 Ki logits are the last kernel's alone: it holds them in LDS and takes the
 // same steps there.
 //
 // Few rows are bound by latency: four launches, each with a chain of two or three loads, scans and barriers (1 x 32000 fp32 with top-p 23.6 us, of
@@ -112,6 +112,52 @@ __device__ __forceinline__ uint32_t key_at(const SampleArgs& a, int row, int i) 
   return logit_key(to_float(static_cast<const T*>(a.logits)[static_cast<size_t>(row) * a.stride + i]));
 }
 
+// The row as pieces of 16 bytes at aligned addresses: element e of them is logit e - shift.
+template <typename T>
+struct RowReader {
+  static constexpr int kPer = 16 / sizeof(T);
+  const T* row;
+  int shift, vocab;
+  __device__ __forceinline__ RowReader(const SampleArgs& a, int r) {
+    row = static_cast<const T*>(a.logits) + static_cast<size_t>(r) * a.stride;
+    shift = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    vocab = a.vocab;
+  }
+  typedef __attribute__((__vector_size__(16))) T Piece;
+  // f(logit, index) for the row's elements e0 .. e0 + kPer, e0 + step .., up to e1 (multiples of kPer), in the order of the indexes; kAhead pieces are
+  // loaded before the first is used.  Only the row's own logits are read; -inf and NaN are passed over, and pieces with nothing from `least` up.
+  template <typename F>
+  __device__ __forceinline__ void each(int e0, int e1, int step, float least, F&& f) const {
+    constexpr int kAhead = 4;
+    for (int e = e0; e < e1; e += kAhead * step) {
+      Piece v[kAhead];
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        const int i = e + a * step - shift;
+        if (i >= 0 && i + kPer <= vocab && e + a * step < e1) v[a] = *reinterpret_cast<const Piece*>(row + i);
+      }
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        const int i = e + a * step - shift;
+        if (e + a * step >= e1) break;
+        const bool whole = i >= 0 && i + kPer <= vocab;
+        if (whole) {
+          float most = to_float(v[a][0]);
+#pragma unroll
+          for (int j = 1; j < kPer; ++j) most = fmaxf(most, to_float(v[a][j]));
+          if (most < least) continue;
+        }
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+          if (!whole && (i + j < 0 || i + j >= vocab)) continue;
+          const float z = to_float(whole ? v[a][j] : row[i + j]);
+          if (z > -INFINITY) f(z, i + j);
+        }
+      }
+    }
+  }
+};
+
 struct Cut {              // the ranks above it: logits above key, and the first `ties` (by index) of those equal to it
   uint32_t key;
   unsigned ties;
@@ -133,6 +179,8 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const R
   unsigned *count = sh.count, *wave_ties = sh.wave_ties, *wave_kept = sh.wave_kept;
   unsigned long long *mass = sh.mass, *wave_mass = sh.wave_mass;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = a.vocab;
+  const RowReader<T> in(a, row);
+  constexpr int kPer = RowReader<T>::kPer;
 
   // ---- radix descent: the cut behind the rank at which the count reaches `want` or the weights in front reach `target`
   unsigned long long set_mass = 0;                     // weights above the cut, its kept ties included
@@ -143,17 +191,17 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const R
     for (int digit = 3; digit >= 0; --digit) {
       if (tid < 256) { count[tid] = 0; mass[tid] = 0; }
       __syncthreads();
-      for (int i = tid; i < n; i += 64 * W) {
-        const uint32_t k = key_at<T>(a, row, i);
-        if (k <= kKeyNone || (digit < 3 && (k >> (8 * digit + 8)) != prefix)) continue;
+      in.each(tid * kPer, n + in.shift, 64 * W * kPer, -INFINITY, [&](float z, int) __attribute__((always_inline)) {
+        const uint32_t k = logit_key(z);
+        if (digit < 3 && (k >> (8 * digit + 8)) != prefix) return;
         // (lanes with one logit add it together: such rows are why this is called, and 64 sums of one place would follow each other)
         const unsigned long long here = __ballot(true);
         const bool one = __ballot(k == static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(k)))) == here;
-        if (one && lane != __builtin_ctzll(here)) continue;
+        if (one && lane != __builtin_ctzll(here)) return;
         const unsigned n_same = one ? __popcll(here) : 1u;
         atomicAdd(&count[(k >> (8 * digit)) & 255], n_same);
         atomicAdd(&mass[(k >> (8 * digit)) & 255], n_same * fixed_of(weight_of(k, top, s.inv_t), a.shift));
-      }
+      });
       __syncthreads();
       if (tid == 0) {
         unsigned c = above;
@@ -195,7 +243,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const R
   }
 
   // ---- the draw, in the order of the indexes: a wavefront owns a contiguous share
-  const int share = (n + W - 1) / W, i0 = wave * share, i1 = min(n, i0 + share);
+  const int share = (n + in.shift + W * kPer - 1) / (W * kPer) * kPer, e0 = wave * share, e1 = min(n + in.shift, e0 + share), i0 = max(e0 - in.shift, 0), i1 = e1 - in.shift;
   auto weight = [&](uint32_t k) {
     const double w = k > kKeyNone ? weight_of(k, top, s.inv_t) : 0.0;
     return w >= s.min_p || k == top ? w : 0.0;
@@ -204,15 +252,14 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const R
   const unsigned long long each = tie_in ? fixed_of(weight(cut.key), a.shift) : 0;
   unsigned kept = 0, ties = 0;
   unsigned long long sum = 0;
-  for (int i = i0 + lane; i < i1; i += 64) {
-    const uint32_t k = key_at<T>(a, row, i);
-    if (k <= kKeyNone) continue;
+  in.each(e0 + lane * kPer, e1, 64 * kPer, -INFINITY, [&](float z, int) __attribute__((always_inline)) {
+    const uint32_t k = logit_key(z);
     if (k == cut.key) ++ties;
     else if (k > cut.key) {
       const double w = weight_of(k, top, s.inv_t);
       if (w >= s.min_p || k == top) { ++kept; sum += fixed_of(w, a.shift); }
     }
-  }
+  });
   for (int o = 32; o > 0; o >>= 1) { kept += __shfl_xor(kept, o, 64); ties += __shfl_xor(ties, o, 64); sum += __shfl_xor(sum, o, 64); }
   if (lane == 0) { wave_ties[wave] = ties; wave_kept[wave] = kept; wave_mass[wave] = sum; }
   __syncthreads();
@@ -238,9 +285,14 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int row, const R
   }
   if (wave != mine) return;
   unsigned seen = first_ties;
-  for (int base = i0; base < i1; base += 64) {
+  constexpr int kNext = 4;                             // (logits that are read ahead)
+  uint32_t next[kNext];
+  for (int base = i0, turn = 0; base < i1; base += 64, turn = (turn + 1) % kNext) {
     const int i = base + lane;
-    const uint32_t k = i < i1 ? key_at<T>(a, row, i) : 0;
+    if (turn == 0)
+#pragma unroll
+      for (int j = 0; j < kNext; ++j) next[j] = i + 64 * j < i1 ? key_at<T>(a, row, i + 64 * j) : 0;
+    const uint32_t k = turn == 0 ? next[0] : turn == 1 ? next[1] : turn == 2 ? next[2] : next[3];
     const bool tie = k > kKeyNone && k == cut.key;
     const unsigned long long tied = __ballot(tie);
     const unsigned rank = seen + __popcll(tied & ((1ull << lane) - 1));
@@ -328,52 +380,6 @@ struct RowScratch {
   unsigned tile_kept[kTiles];
   unsigned n_list, unused[3];
   Cuts cuts;                          // (of a row that needs a cut and has bins)
-};
-
-// The row as pieces of 16 bytes at aligned addresses: element e of them is logit e - shift.
-template <typename T>
-struct RowReader {
-  static constexpr int kPer = 16 / sizeof(T);
-  const T* row;
-  int shift, vocab;
-  __device__ __forceinline__ RowReader(const SampleArgs& a, int r) {
-    row = static_cast<const T*>(a.logits) + static_cast<size_t>(r) * a.stride;
-    shift = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
-    vocab = a.vocab;
-  }
-  typedef __attribute__((__vector_size__(16))) T Piece;
-  // f(logit, index) for the row's elements e0 .. e0 + kPer, e0 + step .., up to e1 (multiples of kPer), in the order of the indexes; kAhead pieces are
-  // loaded before the first is used.  Only the row's own logits are read; -inf and NaN are passed over, and pieces with nothing from `least` up.
-  template <typename F>
-  __device__ __forceinline__ void each(int e0, int e1, int step, float least, F&& f) const {
-    constexpr int kAhead = 4;
-    for (int e = e0; e < e1; e += kAhead * step) {
-      Piece v[kAhead];
-#pragma unroll
-      for (int a = 0; a < kAhead; ++a) {
-        const int i = e + a * step - shift;
-        if (i >= 0 && i + kPer <= vocab && e + a * step < e1) v[a] = *reinterpret_cast<const Piece*>(row + i);
-      }
-#pragma unroll
-      for (int a = 0; a < kAhead; ++a) {
-        const int i = e + a * step - shift;
-        if (e + a * step >= e1) break;
-        const bool whole = i >= 0 && i + kPer <= vocab;
-        if (whole) {
-          float most = to_float(v[a][0]);
-#pragma unroll
-          for (int j = 1; j < kPer; ++j) most = fmaxf(most, to_float(v[a][j]));
-          if (most < least) continue;
-        }
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-          if (!whole && (i + j < 0 || i + j >= vocab)) continue;
-          const float z = to_float(whole ? v[a][j] : row[i + j]);
-          if (z > -INFINITY) f(z, i + j);
-        }
-      }
-    }
-  }
 };
 
 // The row's extremes from its parts: every wavefront for itself.
