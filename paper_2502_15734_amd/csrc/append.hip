@@ -153,13 +153,15 @@ __device__ __forceinline__ void write_rows(const AppendArgs& a, const InvFreq& i
   __syncthreads();                                     // (the workgroup's loads behind it see the rows)
 }
 
-// x as a bf16, or as the sum of two.  Part 0 of two: the upper 16 bits, x becomes the rest; the last part: the nearest bf16.  The rest keeps the sign and
-// is not 0, so that a product with an infinite factor is one infinity and not a difference of two.
-template <int PARTS>
+// x as a bf16, or as the sum of two.  Part 0 of two: the upper 16 bits of the number in front of x (towards 0), x becomes the rest.  So neither part of a number
+// is 0 - a product with an infinite factor is one infinity and not a difference of two or 0 x infinity - and both parts of 0 are: a masked key's
+// weight takes nothing of its value, however large.  The last part: the nearest bf16.  POSITIVE: x has no sign (NaN may).
+template <int PARTS, bool POSITIVE = false>
 __device__ __forceinline__ bf16_t take_part(float& x, int part) {
   if (part == PARTS - 1) return static_cast<bf16_t>(x);
-  const float up = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-  x = copysignf(fmaxf(fabsf(x - up), 0x1p-126f), up);
+  const uint32_t sign = POSITIVE ? 0u : __float_as_uint(x) & 0x80000000u;
+  const float up = __uint_as_float((__builtin_elementwise_sub_sat(__float_as_uint(x) ^ sign, 1u) & 0xffff0000u) | sign);
+  x -= up;
   return static_cast<bf16_t>(up);
 }
 
@@ -199,10 +201,11 @@ template <int D> struct Tile<bf16_t, D> {
   static __device__ __forceinline__ f32x4 add_values(const Piece& v, const Piece& p, f32x4 o) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o, 0, 0, 0);
   }
+  template <bool POSITIVE>
   static __device__ __forceinline__ Piece piece(float (&x)[8], int part) {
     Piece w;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = take_part<2>(x[e], part);
+    for (int e = 0; e < 8; ++e) w[e] = take_part<2, POSITIVE>(x[e], part);
     return w;
   }
 };
@@ -241,6 +244,7 @@ template <int D> struct Tile<float, D> {
     for (int e = 0; e < 4; ++e) o = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], p[e], o, 0, 0, 0);
     return o;
   }
+  template <bool>
   static __device__ __forceinline__ Piece piece(const float (&x)[4], int) { return Piece{x[0], x[1], x[2], x[3]}; }
 };
 
@@ -335,8 +339,8 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
     }
 #pragma unroll
     for (int part = 0; part < Keys::kParts; ++part) {
-      q[part][i] = Keys::piece(x, part);
-      q[part][i + kQ / 2] = Keys::piece(y, part);
+      q[part][i] = Keys::template piece<false>(x, part);
+      q[part][i + kQ / 2] = Keys::template piece<false>(y, part);
     }
   }
 
@@ -383,7 +387,7 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
     if (!apart) {
 #pragma unroll
       for (int part = 0; part < Keys::kParts; ++part) {
-        const Piece w = Keys::piece(p, part);
+        const Piece w = Keys::template piece<true>(p, part);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) o[i] = Keys::add_values(t.v[i], w, o[i]);
       }
@@ -397,7 +401,7 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
         for (int e = 0; e < kTok; ++e) only[e] = n == k ? p[e] : 0.f;
         Piece w[Keys::kParts];
 #pragma unroll
-        for (int part = 0; part < Keys::kParts; ++part) w[part] = Keys::piece(only, part);
+        for (int part = 0; part < Keys::kParts; ++part) w[part] = Keys::template piece<true>(only, part);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
           Piece v = t.v[i];
@@ -648,11 +652,11 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
       float x0 = __builtin_amdgcn_exp2f(s[b][2 * x]), x1 = __builtin_amdgcn_exp2f(s[b][2 * x + 1]);
       l += x0;
       l += x1;
-      w[b][x / 4][2 * x % 8] = take_part<kParts>(x0, 0);
-      w[b][x / 4][2 * x % 8 + 1] = take_part<kParts>(x1, 0);
+      w[b][x / 4][2 * x % 8] = take_part<kParts, true>(x0, 0);
+      w[b][x / 4][2 * x % 8 + 1] = take_part<kParts, true>(x1, 0);
       if constexpr (kParts == 2) {
-        rest[x / 4][2 * x % 8] = take_part<kParts>(x0, 1);
-        rest[x / 4][2 * x % 8 + 1] = take_part<kParts>(x1, 1);
+        rest[x / 4][2 * x % 8] = take_part<kParts, true>(x0, 1);
+        rest[x / 4][2 * x % 8 + 1] = take_part<kParts, true>(x1, 1);
       }
     };
     // S(b); under it the weights of block `under` (-1: none)

@@ -370,6 +370,35 @@ def test_append_attention_values_a_row_does_not_see(dtype, value):
     assert torch.isnan(t["out"][ends].float()).any(-1).all()
 
 
+@pytest.mark.parametrize("dtype,d,new", [("bf16", 128, 3), ("bf16", 64, 4), ("bf16", 128, 6), ("bf16", 64, 16), ("bf16", 128, 16), ("bf16", 128, 21), ("bf16", 64, 30),
+                                         ("f32", 128, 6), ("f32", 64, 21)])
+def test_append_attention_largest_values_a_row_does_not_see(dtype, d, new):
+    """The last new token's values are the type's largest, of either sign: nothing of them is in the rows in front of it (up to 16, up to 64 and more rows
+    times heads of a group)."""
+    b = Batch(14, [((30,), new + 34, new), ((), new, new), ((45,), 9, 1)], 8, 2, d, dtype)
+    most = torch.finfo(b.v_new.dtype).max
+    ends = [new - 1, 2 * new - 1]
+    b.v_new[ends[0]], b.v_new[ends[1]] = most, -most
+    t = b.up()
+    b.call(_ctx(dtype, 8, 2, d), t)
+    torch.cuda.synchronize()
+    b.check(t, hidden=ends)
+
+
+@pytest.mark.parametrize("dtype,d,new", [("bf16", 128, 1), ("bf16", 64, 9), ("bf16", 128, 21), ("f32", 128, 2)])
+def test_append_attention_queries_of_zeros(dtype, d, new):
+    """A pair of the queries is 0 (and -0), the keys' is the type's largest: their product is 0."""
+    b = Batch(15, [((130,), 40, new), ((45,), new + 9, new)], 8, 2, d, dtype)
+    for i in (5, 5 + d // 2):
+        b.q[..., i] = 0.0
+        b.q[:, ::2, i] = -0.0
+        b.k_pool[..., i] = torch.where(torch.isnan(b.k_pool[..., i]), b.k_pool[..., i], torch.finfo(b.q.dtype).max * (1 if i == 5 else -1))
+    t = b.up()
+    b.call(_ctx(dtype, 8, 2, d), t)
+    torch.cuda.synchronize()
+    b.check(t)
+
+
 def test_append_attention_rows_behind_and_no_lse():
     b = Batch(9, SHAPES["draft"], 8, 2, 128, "bf16")
     ctx = _ctx()
