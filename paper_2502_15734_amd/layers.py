@@ -16,6 +16,7 @@ Argument marshalling and call order only; every step runs in libcachecraft.
 """
 from __future__ import annotations
 
+import math
 from typing import Callable, List, Optional, Sequence
 
 import numpy as np
@@ -258,6 +259,8 @@ class AnswerLoop:
         self.b.ctx.sample(self.logits, self.logits.shape[1], self.u, self.token, logprob=self.logprob, n_kept=self.n_kept, workspace=self.ws,
                           **self.settings)
         self.token.masked_fill_(~self.alive, -1)
+        self.logprob.masked_fill_(~self.alive, -math.inf)
+        self.n_kept.masked_fill_(~self.alive, 0)
         if self.stop is not None:
             self.alive &= self.token != self.stop
 
@@ -288,7 +291,7 @@ class AnswerLoop:
 
     def run(self, u, graph: bool = False, keep: bool = False):
         """u [steps, requests]: the uniform numbers the tokens are drawn with (at most answer_tokens + 1 steps in all).  Returns the tokens [steps,
-        requests] (-1: none) and their log-probabilities; with keep also the logits each was drawn from."""
+        requests] (-1: none) and their log-probabilities (-infinity there); with keep also the logits each was drawn from."""
         u = torch.as_tensor(np.ascontiguousarray(u, dtype=np.float32)).to(self.u.device)
         if self.drawn + u.shape[0] > self.loop.answer_tokens + 1:
             raise ValueError("AnswerLoop: more tokens than the pages have room for")

@@ -755,3 +755,23 @@ def test_answer_loop_stops(graph):
         assert np.array_equal(got[:n, r], free[:n, r]) and (got[n:, r] == -1).all()
     assert (got[7:, 1] == -1).all()
     loop.close()
+
+
+def _ended(got, logprobs, free, r, n):
+    """Request r's tokens are those of the free run up to step n, and nothing from there on."""
+    assert np.array_equal(got[:n, r], free[:n, r]) and (got[n:, r] == -1).all()
+    assert np.isfinite(logprobs[:n, r]).all() and np.isneginf(logprobs[n:, r]).all()
+
+
+def test_answer_loop_log_probabilities_of_stopped_requests():
+    u = np.random.default_rng(5).random((16, 3), dtype=np.float32)
+    _, _, loop, ans, _, _ = _answer_setup("f32", temperature=1.0)
+    free, _ = ans.run(u)
+    loop.close()
+    stop = int(free[6, 1])
+    _, _, loop, ans, _, _ = _answer_setup("f32", temperature=1.0, stop=stop)
+    got, logprobs = ans.run(u)
+    for r in range(3):
+        at = np.nonzero(free[:, r] == stop)[0]
+        _ended(got, logprobs, free, r, int(at[0]) + 1 if len(at) else len(free))
+    loop.close()
