@@ -192,7 +192,7 @@ class AnswerLoop:
     cc_append_attention over the layer's pages -> cc_linear -> cc_rms_norm -> cc_gated_linear -> cc_linear, -> logits.
     embed [vocab, hidden], gain_out [hidden], w_out [vocab, hidden]: embedding, last normalisation, output projection (numpy).
     temperature, top_k, top_p, min_p: one value, or one per request; None: off.  stop: a request that draws this token
-    gets no further one.  Nothing of a step depends on the host, so graph=True captures one and replays it."""
+    gets no further one; neither does one whose logits are all -infinity or NaN.  Nothing of a step depends on the host, so graph=True captures one and replays it."""
 
     def __init__(self, loop: DecoderLoop, embed, gain_out, w_out, eps: float = 1.0e-5, temperature=None, top_k=None, top_p=None,
                  min_p=None, stop: Optional[int] = None):
@@ -255,10 +255,11 @@ class AnswerLoop:
         c.linear(self.x, self.w_out, self.logits, workspace=self.ws_products)
 
     def _draw(self):
-        """The next token of every request from the logits; -1 for those that have stopped."""
+        """The next token of every request from the logits; -1 for those that have ended, or whose logits hold nothing to draw: they end here."""
         self.b.ctx.sample(self.logits, self.logits.shape[1], self.u, self.token, logprob=self.logprob, n_kept=self.n_kept, workspace=self.ws,
                           **self.settings)
         self.token.masked_fill_(~self.alive, -1)
+        self.alive &= self.token >= 0
         self.logprob.masked_fill_(~self.alive, -math.inf)
         self.n_kept.masked_fill_(~self.alive, 0)
         if self.stop is not None:
@@ -291,7 +292,7 @@ class AnswerLoop:
 
     def run(self, u, graph: bool = False, keep: bool = False):
         """u [steps, requests]: the uniform numbers the tokens are drawn with (at most answer_tokens + 1 steps in all).  Returns the tokens [steps,
-        requests] (-1: none) and their log-probabilities (-infinity there); with keep also the logits each was drawn from."""
+        requests] (-1: none, as the request has ended) and their log-probabilities (-infinity there); with keep also the logits each was drawn from."""
         u = torch.as_tensor(np.ascontiguousarray(u, dtype=np.float32)).to(self.u.device)
         if self.drawn + u.shape[0] > self.loop.answer_tokens + 1:
             raise ValueError("AnswerLoop: more tokens than the pages have room for")

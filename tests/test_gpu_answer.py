@@ -775,3 +775,27 @@ def test_answer_loop_log_probabilities_of_stopped_requests():
         at = np.nonzero(free[:, r] == stop)[0]
         _ended(got, logprobs, free, r, int(at[0]) + 1 if len(at) else len(free))
     loop.close()
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_answer_loop_ends_where_nothing_can_be_drawn(graph):
+    """A token whose embedding is NaN: the logits behind it are all NaN, and the request gets -1 and nothing more; the others go on."""
+    u = np.random.default_rng(6).random((14, 3), dtype=np.float32)
+    _, _, loop, ans, _, _ = _answer_setup("f32", temperature=1.0)
+    free, _ = ans.run(u)
+    loop.close()
+    bad = int(free[4, 1])
+    _, _, loop, ans, _, _ = _answer_setup("f32", temperature=1.0)
+    ans.embed[bad] = math.nan
+    got, logprobs = ans.run(u, graph=graph)
+    for r in range(3):
+        at = np.nonzero(free[:, r] == bad)[0]
+        _ended(got, logprobs, free, r, int(at[0]) + 1 if len(at) else len(free))
+    assert (got[5:, 1] == -1).all() and int(ans.n_kept[1]) == 0
+    loop.close()
+    _, _, loop, ans, _, _ = _answer_setup("f32", temperature=1.0)
+    ans.logits[1] = -math.inf                                            # ... and a prompt that leaves nothing
+    got, logprobs = ans.run(u, graph=graph)
+    for r in range(3):
+        _ended(got, logprobs, free, r, 0 if r == 1 else len(free))
+    loop.close()
