@@ -192,7 +192,7 @@ class AnswerLoop:
     cc_append_attention over the layer's pages -> cc_linear -> cc_rms_norm -> cc_gated_linear -> cc_linear, -> logits.
     embed [vocab, hidden], gain_out [hidden], w_out [vocab, hidden]: embedding, last normalisation, output projection (numpy).
     temperature, top_k, top_p, min_p: one value, or one per request; None: off.  stop: a request that draws this token
-    gets no further one; neither does one whose logits are all -infinity or NaN.  Nothing of a step depends on the host, so graph=True captures one and replays it."""
+    gets no further one; neither does one whose logits are all -infinity or NaN, or for which no row is left.  Nothing of a step depends on the host, so graph=True captures one and replays it."""
 
     def __init__(self, loop: DecoderLoop, embed, gain_out, w_out, eps: float = 1.0e-5, temperature=None, top_k=None, top_p=None,
                  min_p=None, stop: Optional[int] = None):
@@ -271,6 +271,7 @@ class AnswerLoop:
         self.n_new.index_copy_(0, self.last_seg, self.alive.int())
         c.extend_segments(self.segs, self.n_new, self.tab_cap, b.req_seg_off, self.free_left, self.block_tab, b.k_req.shape[0], self.segs, self.cu_q,
                           self.q_pos, self.slot_map, self.row_req, self.last_row, self.status, self.counts, self.ws)
+        self.alive &= self.status == 0                                # (one that got no row has no logits either)
         # (the pages taken leave the list: what is left moves to its front, the end repeats its last entry and is never reached)
         left = torch.arange(self.free.shape[0], device=self.free.device) + self.counts[1]
         self.free_left.copy_(self.free_left[left.clamp(max=self.free.shape[0] - 1)])

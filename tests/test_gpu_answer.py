@@ -799,3 +799,19 @@ def test_answer_loop_ends_where_nothing_can_be_drawn(graph):
     for r in range(3):
         _ended(got, logprobs, free, r, 0 if r == 1 else len(free))
     loop.close()
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_answer_loop_ends_where_no_row_is_left(graph):
+    """A request whose table is full gets nothing from then on, whatever logits an earlier step left."""
+    u = np.random.default_rng(7).random((9, 3), dtype=np.float32)
+    _, _, loop, ans, _, _ = _answer_setup("f32", temperature=1.0)
+    free, _ = ans.run(u)
+    loop.close()
+    for r, n in ((1, 1), (2, 9)):                                       # (a question of 16 tokens fills its page, one of 3 has room for 13 more)
+        _, _, loop, ans, _, _ = _answer_setup("f32", temperature=1.0)
+        ans.tab_cap[ans.last_seg[r]] = 1
+        got, logprobs = ans.run(u, graph=graph)
+        for i in range(3):
+            _ended(got, logprobs, free, i, n if i == r else 9)
+        loop.close()
