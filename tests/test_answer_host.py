@@ -124,3 +124,16 @@ def test_calls_beyond_the_grid_are_refused(lib):
     assert lib.cc_append_attention(h, good, good, good, None, good, good, good, 1 << 18, 1 << 17, good, good, 8, good, good, 65535, good, 65535, 4000, 1,
                                    None, C.c_void_p(8192), None, good, 1 << 60, None) == -1 and b"2^24 - 1 workgroups" in lib.cc_last_error(h)
     ctx.close()
+
+
+def test_refused_workspaces_of_rows_in_parts(lib):
+    """cc_sample over a vocabulary whose rows are read in parts (those that one workgroup holds need no workspace)."""
+    import paper_2502_15734_amd as P
+    ctx = P.Context(8, 2, 128, 5.0e5, P.CC_BF16)
+    h, good, odd = ctx._h, C.c_void_p(4096), C.c_void_p(4100)
+    need = lib.cc_sample_workspace_bytes(h, 4, 32000)
+    assert need > 0 and 2 * need - 256 <= lib.cc_sample_workspace_bytes(h, 8, 32000) <= 2 * need and lib.cc_sample_workspace_bytes(None, 4, 32000) == 0
+    call = lambda ws, n: lib.cc_sample(h, good, 0, 4, 32000, 32000, None, None, None, None, good, good, None, None, ws, n, None)
+    for ws, n, status in ((None, need, -1), (odd, need, -1), (good, need - 1, -3), (good, 0, -3)):
+        assert call(ws, n) == status and b"cc_sample" in lib.cc_last_error(h)
+    ctx.close()

@@ -461,6 +461,46 @@ def test_append_attention_values_in_the_store(dtype):
     b.check(t, v_of=lambda p: st[int(after[p])] if int(after[p]) >= 0 else v[p])
 
 
+@pytest.mark.parametrize("value", [None, float("inf"), float("nan")])
+@pytest.mark.parametrize("d,new", [(128, 5), (64, 5), (128, 16), (128, 40), (64, 40)])
+def test_append_attention_many_rows_with_values_in_the_store(d, new, value):
+    """As above with 17 rows times heads of a group and more (up to 64, and more), bf16.  value: of the last new token, which only its own row sees."""
+    b = Batch(17, [((100, 50), 40 + new, new), ((64, 400), 5 + new, new), ((33,), 9, 1)], 8, 2, d, "bf16")
+    ends = [new - 1, 2 * new - 1] if value is not None else []
+    b.v_new[ends] = 0.0 if value is None else value
+    t = b.up()
+    store = torch.randn(b.n_blocks, 2, d, 16, generator=torch.Generator().manual_seed(3)).to(b.q.dtype).cuda()
+    rng = np.random.default_rng(4)
+    v_map = np.full(b.n_blocks, -1)
+    pages = set(int(p) for p in b.tab[::2]) | {int(b.slot[0]) // 16, int(b.slot[new]) // 16}            # (the first pages that get rows among them)
+    for p in pages:
+        v_map[p] = rng.integers(0, b.n_blocks)
+    before = v_map.copy()
+    dev_map = _i32(v_map)
+    b.call(_ctx("bf16", 8, 2, d), t, shared=(store, dev_map))
+    torch.cuda.synchronize()
+    after, st = _np(dev_map), store.float().cpu().numpy()
+    written = set(int(s) // 16 for s in b.slot)
+    assert np.array_equal(after, [-1 if p in written else before[p] for p in range(b.n_blocks)])
+    b.check(t, v_of=lambda p: st[after[p]] if after[p] >= 0 else t["v_pool"][p].float().cpu().numpy(), hidden=ends)
+
+
+@pytest.mark.parametrize("dtype,d,new", [("bf16", 64, 1), ("bf16", 128, 8), ("bf16", 64, 32), ("bf16", 128, 20), ("bf16", 64, 40), ("bf16", 128, 64), ("f32", 64, 8), ("f32", 128, 20)])
+def test_append_attention_over_more_pages_than_are_listed_at_a_time(dtype, d, new):
+    """One range of keys of more than 256 pages per request (64 requests on 8 KV heads are not divided): new rows on both sides of the 256th page, behind it in
+    a segment of its own, and behind two short ones; the last one's values are not finite and seen by its own row alone."""
+    b = Batch(18, [((), 4096 + (new + 1) // 2, new), ((4096,), new, new), ((1500, 4, 0, 3000, 1), new + 20, new)] + [((), 1 + i % 5, 1) for i in range(61)], 16, 8, d, dtype)
+    ctx = _ctx(dtype, 16, 8, d)
+    rows = len(b.pos)
+    assert ctx.append_attention_workspace_bytes(rows, b.most, b.n_req, b.max_ctx, b.max_segs) < 4 * rows * (16 * (d + 2) + 1) + 256          # (one part per row and head)
+    ends = [new - 1, 2 * new - 1, 3 * new - 1] if new > 1 else []
+    b.v_new[ends] = float("inf")
+    t = b.up()
+    b.call(ctx, t)
+    torch.cuda.synchronize()
+    b.check(t, hidden=ends)
+
+
 def test_append_attention_in_graphs_that_share_a_workspace():
     """Two captured calls over one workspace, replayed in turn beside eager work, on a stream of their own."""
     batches = [Batch(12, SHAPES["draft"] + [((3000,), 4, 1)], 8, 2, 128, "bf16"), Batch(13, SHAPES["one each"], 8, 2, 128, "bf16")]
@@ -600,6 +640,29 @@ def test_sample_values_that_are_not_finite(vocab):
     for s in (dict(), dict(top_k=np.full(8, 2)), dict(top_p=np.full(8, 0.6)), dict(temperature=np.zeros(8)), dict(min_p=np.full(8, 0.5)),
               dict(top_k=np.full(8, 150), top_p=np.full(8, 0.9), min_p=np.full(8, 0.01), temperature=np.full(8, 0.7))):
         for u in (rng.random(8, dtype=np.float32), np.full(8, 1 - 2.0 ** -24, np.float32), np.full(8, 1.0), np.full(8, np.nan), np.full(8, -0.5)):
+            _check_sample(_sample(_ctx(), z, vocab, u, **s), z, vocab, u, **s)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [12279, 40001, 128256])
+def test_sample_values_that_are_not_finite_in_long_rows(vocab, dtype):
+    """As above for the largest vocabulary that is held at once (an odd one) and for rows in parts; whole parts without a logit, too."""
+    rng = np.random.default_rng(vocab)
+    z = torch.from_numpy(rng.standard_normal((9, vocab)).astype(np.float32))
+    z[0] = -math.inf
+    z[1] = math.nan
+    z[2, ::2] = math.nan
+    z[3, 1::2] = -math.inf
+    z[4, [5, 17, vocab - 2]] = math.inf
+    z[5, 7] = math.inf
+    z[6] = torch.where(torch.arange(vocab) == vocab - 1, 0.5, -math.inf)
+    z[7, :vocab - 3000] = -math.inf
+    z[8, 3000:] = math.nan
+    z = z.to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda()
+    full = np.ones(9)
+    for s in (dict(), dict(top_k=2 * np.ones(9, int)), dict(top_p=0.6 * full), dict(temperature=0 * full), dict(min_p=0.5 * full),
+              dict(top_k=150 * np.ones(9, int), top_p=0.9 * full, min_p=0.01 * full, temperature=0.7 * full)):
+        for u in (rng.random(9, dtype=np.float32), np.full(9, 1 - 2.0 ** -24, np.float32), np.full(9, np.nan)):
             _check_sample(_sample(_ctx(), z, vocab, u, **s), z, vocab, u, **s)
 
 
