@@ -22,6 +22,7 @@
 // row over 130 000 tokens 105 us (5.1 TB/s), one over 700 tokens 12.7 us, of which two launches take 5 and the chain of dependent loads (segments, page
 // table, page, parts) most of the rest.
 #include <algorithm>
+#include <cstddef>
 #include <type_traits>
 
 #include "device_util.h"
@@ -71,7 +72,12 @@ __device__ __forceinline__ int list_pages(const AppendArgs& a, int s_begin, int 
   for (int s0 = s_begin; s0 < s_end; s0 += 256) {
     const int s = s0 + tid;
     int4 mine{0, 0, 0, 0};
-    if (s < s_end) mine = *reinterpret_cast<const int4*>(&a.segs[s].logical_start);     // start, tokens, table offset, (rows)
+    if (s < s_end) {                                              // start, tokens; table offset, (rows)
+      static_assert(offsetof(cc_segment, logical_start) % alignof(int2) == 0 && sizeof(cc_segment) % alignof(int2) == 0, "these pieces are aligned");
+      const int2* at = reinterpret_cast<const int2*>(&a.segs[s].logical_start);
+      const int2 head = at[0], tail = at[1];
+      mine = make_int4(head.x, head.y, tail.x, tail.y);
+    }
     const int n = pages_of(mine.y);
     if (s == s_end - 1) *end_pos = mine.x + max(mine.y, 0);
     int end = n;
