@@ -486,6 +486,8 @@ int cc_chunk_attention(cc_ctx* ctx, const void* q, const int32_t* q_pos, const i
  *       or the pages / rows of all requests up to and including it (the refused ones' wishes count) exceed
  *       n_free / max_rows.  A request that needs no page is not refused for pages.
  *   counts [4]: rows, pages taken, requests refused, tokens of all segments (must stay below 2^31).
+ *   An empty batch (n_requests = n_segs = 0) has cu_q[0] = 0, counts of 0 and rows of nothing.  Segments without requests
+ *   (n_requests = 0 alone): nothing is written.
  *   workspace: cc_extend_segments_workspace_bytes(ctx, n_segs, n_requests). */
 enum { CC_EXTEND_OK = 0, CC_EXTEND_NO_PAGES = 1, CC_EXTEND_TABLE_FULL = 2, CC_EXTEND_ORDER = 3, CC_EXTEND_NO_ROWS = 4 };
 size_t cc_extend_segments_workspace_bytes(const cc_ctx* ctx, int32_t n_segs, int32_t n_requests);

@@ -658,13 +658,14 @@ int cc_extend_segments(cc_ctx* ctx, const cc_segment* segs_in, const int32_t* n_
   CC_REQUIRE(n_segs <= 65535 && n_requests <= 65535, "more than 65535 segments or requests in one call");
   CC_REQUIRE(n_blocks <= (1 << 27) - 1, "a pool of more than 2^27 - 1 blocks has slots beyond 32 bits");
   CC_REQUIRE(max_rows <= (1 << 30), "more than 2^30 rows in one call");
-  if (n_requests == 0) return CC_OK;
-  CC_REQUIRE(req_seg_off && cu_q && last_row && status && counts, "null pointer");
+  if (n_requests == 0 && n_segs > 0) return CC_OK;
+  CC_REQUIRE(cu_q && counts && (n_requests == 0 || (req_seg_off && last_row && status)), "null pointer");
   CC_REQUIRE(n_segs == 0 || (segs_in && segs && n_new && tab_cap), "null pointer");
   CC_REQUIRE((n_free == 0 || free_blocks) && (n_tab == 0 || block_tab) && (max_rows == 0 || (q_pos && slot_map && row_req)), "null pointer");
   CC_REQUIRE(aligned16(segs_in) && aligned16(segs), "segment tables must be 16-byte aligned");
-  CC_REQUIRE(workspace != nullptr && aligned16(workspace), "workspace missing or misaligned");
-  if (workspace_bytes < cc_extend_segments_workspace_bytes(ctx, n_segs, n_requests))
+  const size_t need = cc_extend_segments_workspace_bytes(ctx, n_segs, n_requests);
+  CC_REQUIRE(need == 0 || (workspace != nullptr && aligned16(workspace)), "workspace missing or misaligned");
+  if (workspace_bytes < need)
     return fail(ctx, CC_ERR_WORKSPACE_TOO_SMALL, "cc_extend_segments: workspace smaller than cc_extend_segments_workspace_bytes()");
   cc::launch_extend_segments(segs_in, n_new, tab_cap, n_segs, req_seg_off, n_requests, free_blocks, n_free, block_tab, n_tab, n_blocks, segs,
                              cu_q, q_pos, slot_map, row_req, max_rows, last_row, status, counts, workspace, static_cast<hipStream_t>(stream));

@@ -9,6 +9,8 @@
 // places the segments (every workgroup scans all needs again, which is cheaper than a launch between) and one for the rows.
 // 32 requests of one row each (5 to 10 segments) 7.5 us, where a launch alone takes 2.4; 250 requests, some with a question, 13.8; the tables of 500 whole
 // prompts, 2.8 million rows, 22 us (1.6 TB/s, of which a third is the chain through the two kernels in front).
+#include <algorithm>
+
 #include "device_util.h"
 
 namespace cc {
@@ -489,14 +491,14 @@ void launch_extend_segments(const cc_segment* segs_in, const int32_t* n_new, con
                             int max_rows, int32_t* last_row, int32_t* status, int32_t* counts, void* workspace, hipStream_t stream) {
   const ExtendArgs a{segs_in, n_new, tab_cap, req_seg_off, free_blocks, block_tab, n_segs, n_requests, n_free, n_tab, n_blocks, max_rows,
                      segs, cu_q, q_pos, slot_map, row_req, last_row, status, counts, aligned16(q_pos) && aligned16(slot_map) && aligned16(row_req)};
-  const int waves = small_waves(n_segs, n_requests, max_rows);
+  const int waves = n_requests > 0 ? small_waves(n_segs, n_requests, max_rows) : 0;
   if (waves == 4) hipLaunchKernelGGL(extend_small_kernel<4>, dim3(1), dim3(256), 0, stream, a);
   if (waves == 16) hipLaunchKernelGGL(extend_small_kernel<16>, dim3(1), dim3(1024), 0, stream, a);
   if (waves != 0) return;
   Need* need = static_cast<Need*>(workspace);
   int32_t* page0 = reinterpret_cast<int32_t*>(need + n_requests);
-  const dim3 per_request((n_requests + 15) / 16);
-  hipLaunchKernelGGL(extend_need_kernel, per_request, dim3(256), 0, stream, a, need);
+  const dim3 per_request(std::max(1, (n_requests + 15) / 16));        // (no request: the totals, and rows of nothing)
+  if (n_requests > 0) hipLaunchKernelGGL(extend_need_kernel, per_request, dim3(256), 0, stream, a, need);
   hipLaunchKernelGGL(extend_segments_kernel, per_request, dim3(256), 0, stream, a, need, page0);
   if (max_rows > 0) hipLaunchKernelGGL(extend_rows_kernel, dim3((max_rows + 256 * kRowsPer - 1) / (256 * kRowsPer)), dim3(256), 0, stream, a, page0);
 }

@@ -137,3 +137,15 @@ def test_refused_workspaces_of_rows_in_parts(lib):
     for ws, n, status in ((None, need, -1), (odd, need, -1), (good, need - 1, -3), (good, 0, -3)):
         assert call(ws, n) == status and b"cc_sample" in lib.cc_last_error(h)
     ctx.close()
+
+
+def test_refused_arguments_of_an_empty_batch(lib):
+    import paper_2502_15734_amd as P
+    ctx = P.Context(8, 2, 128, 5.0e5, P.CC_BF16)
+    h, good = ctx._h, C.c_void_p(4096)
+    assert lib.cc_extend_segments_workspace_bytes(h, 0, 0) == 0
+    for lacking in ("cu", "counts", "pos", "slot", "req"):
+        p = {k: None if k == lacking else good for k in ("cu", "pos", "slot", "req", "counts")}
+        assert lib.cc_extend_segments(h, None, None, None, 0, None, 0, None, 0, None, 0, 8, None, p["cu"], p["pos"], p["slot"], p["req"], 5, None, None,
+                                      p["counts"], None, 0, None) == -1 and b"cc_extend_segments" in lib.cc_last_error(h)
+    ctx.close()

@@ -103,6 +103,15 @@ def test_extend_segments(case, spare, lacking, holes):
     _check_extend(o, t, max_rows)
 
 
+@pytest.mark.parametrize("max_rows", [0, 5, 30000])
+def test_extend_segments_of_an_empty_batch(max_rows):
+    """No request: counts of 0 and rows of nothing, whatever an earlier step left there."""
+    t = Tables(1, 1, 1, 0, 1)
+    t.segs, t.new, t.cap, t.off, t.tab = np.zeros((0, 8), int), np.zeros(0, int), np.zeros(0, int), np.zeros(1, int), np.arange(4)
+    o, _ = _extend(_ctx(), t, max_rows)
+    _check_extend(o, t, max_rows)
+
+
 def test_extend_segments_many_rows():
     """Tables of prompts from nothing whose rows need many workgroups."""
     t = Tables(20, 90, 12, 0, 1500, grow_all=True)
