@@ -508,8 +508,9 @@ int cc_extend_segments(cc_ctx* ctx, const cc_segment* segs_in, const int32_t* n_
  *   lse = -infinity.
  *   What lies in a masked place (padding slots, keys behind the row, pages outside the pool) changes nothing, NaN
  *   and infinities included.
- *   max_q_per_req: at least the rows of any request (host scalar; bounds the grid: a call that would need 2^24 workgroups
- *   or more is refused).
+ *   max_q_per_req: at least the rows of any request (host scalar; bounds the grid).  A call that would need 2^24 workgroups
+ *   or more in a launch is refused: for the attention, for rows to write (one for four), or to join parts (one for
+ *   1024 / d rows and heads, each where a request's keys are divided by more than eight).
  *   max_ctx_tokens, max_segs_per_req: tokens and segments of the largest request (host scalars, upper bounds; they
  *   decide how the keys are divided, not what is read).  lse may be NULL; shared as for cc_sparse_prefill.
  *   The sums' order depends on n_requests, max_q_per_req, max_ctx_tokens and max_segs_per_req, on nothing else.

@@ -699,8 +699,8 @@ int cc_append_attention(cc_ctx* ctx, const void* q, const void* k_new, const voi
   CC_REQUIRE(aligned16(q) && aligned16(k_new) && aligned16(v_new) && aligned16(k_pool) && aligned16(v_pool) && aligned16(out) && aligned16(segs),
              "tensors must be 16-byte aligned");
   CC_REQUIRE(q != out, "q and out must not be the same tensor");
-  CC_REQUIRE(cc::append_groups(ctx, max_q_per_req, n_requests, max_ctx_tokens, max_segs_per_req) < (1 << 24),
-             "more than 2^24 - 1 workgroups: max_q_per_req x n_requests is too large for one call");
+  CC_REQUIRE(cc::append_groups(ctx, n_q_tot, max_q_per_req, n_requests, max_ctx_tokens, max_segs_per_req) < (1 << 24),
+             "more than 2^24 - 1 workgroups: max_q_per_req x n_requests or n_q_tot x heads is too large for one call");
   const size_t need = cc_append_attention_workspace_bytes(ctx, n_q_tot, max_q_per_req, n_requests, max_ctx_tokens, max_segs_per_req);
   CC_REQUIRE(need == 0 || (workspace != nullptr && aligned16(workspace)), "workspace missing or misaligned");
   if (workspace_bytes < need)

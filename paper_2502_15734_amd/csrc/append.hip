@@ -26,6 +26,7 @@
 #include <type_traits>
 
 #include "device_util.h"
+#include "scatter.h"
 
 namespace cc {
 
@@ -1037,8 +1038,18 @@ __global__ __launch_bounds__(64) void append_scalar_kernel(
   if (lse != nullptr && lane == 0) lse[static_cast<size_t>(j) * hq + h] = z == 0.f ? -INFINITY : m + logf(z);
 }
 
-long long append_groups(const cc_ctx* ctx, int max_q_per_req, int n_requests, int max_ctx_tokens, int max_segs_per_req) {
-  return plan_append(ctx, max_q_per_req, n_requests, max_ctx_tokens, max_segs_per_req).groups;
+// Join of the ranges: up to eight by as many rows and heads a workgroup as it has groups of D / 4 threads, more by a workgroup each.
+static bool join_is_wide(const AppendPlan& p) { return p.n_splits > 8; }
+static long long join_groups(const AppendPlan& p, long long n_items, int d) {
+  const int per = join_is_wide(p) ? 1 : 1024 / d;
+  return p.n_splits > 1 ? (n_items + per - 1) / per : 0;
+}
+
+long long append_groups(const cc_ctx* ctx, int n_q_tot, int max_q_per_req, int n_requests, int max_ctx_tokens, int max_segs_per_req) {
+  const long long rows = n_q_tot < 1 << 30 ? scatter_groups(n_q_tot) : n_q_tot;
+  if (ctx->impl == CC_IMPL_SCALAR) return std::max(rows, (n_q_tot + 3ll) / 4);          // (workgroups of a quarter of the threads)
+  const AppendPlan p = plan_append(ctx, max_q_per_req, n_requests, max_ctx_tokens, max_segs_per_req);
+  return std::max({rows, p.groups, join_groups(p, static_cast<long long>(n_q_tot) * ctx->cfg.n_q_heads, ctx->cfg.head_dim)});
 }
 
 size_t append_bytes(const cc_ctx* ctx, int n_q_tot, int max_q_per_req, int n_requests, int max_ctx_tokens, int max_segs_per_req) {
@@ -1059,8 +1070,9 @@ static void launch_append_t(const cc_ctx* ctx, const AppendArgs& a, const Append
     if (p.cols == 128 && shared) hipLaunchKernelGGL((append_tile_kernel<D, 4, true>), grid, dim3(256), 0, stream, a, ctx->inv_freq);
   }
   const int n_items = n_q_tot * a.hq;
-  if (p.n_splits > 8) hipLaunchKernelGGL((append_join_kernel<T, D, true>), dim3(n_items), dim3(256), 0, stream, a, n_items);
-  else if (p.n_splits > 1) hipLaunchKernelGGL((append_join_kernel<T, D, false>), dim3((n_items + 1024 / D - 1) / (1024 / D)), dim3(256), 0, stream, a, n_items);
+  const dim3 join(static_cast<unsigned>(join_groups(p, n_items, D)));
+  if (p.n_splits > 1 && join_is_wide(p)) hipLaunchKernelGGL((append_join_kernel<T, D, true>), join, dim3(256), 0, stream, a, n_items);
+  else if (p.n_splits > 1) hipLaunchKernelGGL((append_join_kernel<T, D, false>), join, dim3(256), 0, stream, a, n_items);
 }
 
 void launch_append_attention(const cc_ctx* ctx, const void* q, const int32_t* src_rows, const int32_t* q_pos, const int32_t* cu_q, int n_q_tot,

@@ -187,7 +187,7 @@ void launch_extend_segments(const cc_segment* segs_in, const int32_t* n_new, con
                             const int32_t* req_seg_off, int n_requests, const int32_t* free_blocks, int n_free, int32_t* block_tab,
                             int n_tab, int n_blocks, cc_segment* segs, int32_t* cu_q, int32_t* q_pos, int32_t* slot_map, int32_t* row_req,
                             int max_rows, int32_t* last_row, int32_t* status, int32_t* counts, void* workspace, hipStream_t stream);
-long long append_groups(const cc_ctx* ctx, int max_q_per_req, int n_requests, int max_ctx_tokens, int max_segs_per_req);      // workgroups of a call
+long long append_groups(const cc_ctx* ctx, int n_q_tot, int max_q_per_req, int n_requests, int max_ctx_tokens, int max_segs_per_req);   // workgroups of 256 threads of a call's largest launch
 size_t append_bytes(const cc_ctx* ctx, int n_q_tot, int max_q_per_req, int n_requests, int max_ctx_tokens, int max_segs_per_req);
 // (scatter: the new rows, written in front of the attention or by it)
 void launch_append_attention(const cc_ctx* ctx, const void* q, const int32_t* src_rows, const int32_t* q_pos, const int32_t* cu_q, int n_q_tot,

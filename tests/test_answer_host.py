@@ -149,3 +149,23 @@ def test_refused_arguments_of_an_empty_batch(lib):
         assert lib.cc_extend_segments(h, None, None, None, 0, None, 0, None, 0, None, 0, 8, None, p["cu"], p["pos"], p["slot"], p["req"], 5, None, None,
                                       p["counts"], None, 0, None) == -1 and b"cc_extend_segments" in lib.cc_last_error(h)
     ctx.close()
+
+
+def test_row_lists_beyond_the_grid_are_refused(lib):
+    """Lists whose rows, or whose parts to join, a launch could not count."""
+    import paper_2502_15734_amd as P
+    ctx = P.Context(8, 2, 128, 5.0e5, P.CC_BF16)
+    h, good = ctx._h, C.c_void_p(4096)
+    call = lambda n, tokens: lib.cc_append_attention(h, good, good, good, None, good, good, good, n, 1, good, good, 8, good, good, 1, good, 1, tokens, 1, None,
+                                                     C.c_void_p(8192), None, good, (1 << 63) - 1, None)
+    for impl, n, tokens in ((P.CC_IMPL_AUTO, 1 << 21, 16000),         # 2^24 rows and heads in 125 ranges: a workgroup each
+                            (P.CC_IMPL_AUTO, 1 << 24, 300),           # 2^27 in two or three: one for eight
+                            (P.CC_IMPL_AUTO, 1 << 26, 100),           # 2^26 rows to write: one for four
+                            (P.CC_IMPL_SCALAR, 1 << 26, 100)):
+        ctx.set_impl(impl)
+        assert call(n, tokens) == -1 and b"2^24 - 1 workgroups" in lib.cc_last_error(h), (impl, n)
+    ctx.close()
+    one = P.Context(1, 1, 128, 5.0e5, P.CC_BF16)
+    assert lib.cc_append_attention(one._h, good, good, good, None, good, good, good, (1 << 31) - 1, 1, good, good, 8, good, good, 1, good, 1, 100, 1, None,
+                                   C.c_void_p(8192), None, good, (1 << 63) - 1, None) == -1 and b"2^24 - 1 workgroups" in lib.cc_last_error(one._h)
+    one.close()
