@@ -503,7 +503,8 @@ int cc_extend_segments(cc_ctx* ctx, const cc_segment* segs_in, const int32_t* n_
  * arguments (rows, positions and slots from cc_extend_segments or any list cc_sparse_prefill takes), but the KEYS are
  * divided over workgroups, and the parts joined, so that a few rows of a long context fill the chip.
  *   slot_map[j] is the slot of row j's own token, in a page of its request, or lies outside the pool: the row is then
- *   attended but not written.  Rows [cu_q[n_requests], n_q_tot) are not attended, their out and lse stay as they are, and
+ *   attended but not written.  As for cc_sparse_prefill the rows of one page follow each other (one that is not written
+ *   parts them: cc_check_query_list).  Rows [cu_q[n_requests], n_q_tot) are not attended, their out and lse stay as they are, and
  *   their slots lie outside the pool (cc_extend_segments leaves them so).  A row that sees no key gets zeros and
  *   lse = -infinity.
  *   What lies in a masked place (padding slots, keys behind the row, pages outside the pool) changes nothing, NaN

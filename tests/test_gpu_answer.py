@@ -510,6 +510,33 @@ def test_append_attention_over_more_pages_than_are_listed_at_a_time(dtype, d, ne
     b.check(t, hidden=ends)
 
 
+@pytest.mark.parametrize("dtype,d,new", [("bf16", 128, 3), ("bf16", 64, 9), ("bf16", 128, 30), ("f32", 64, 2), ("f32", 128, 25)])
+def test_append_attention_rows_that_are_attended_and_not_written(dtype, d, new):
+    """Slots outside the pool, on either side: the row sees what its page holds already; the pages stay as they are but for the other rows' slots.  (Rows
+    that are written and lie in one page follow each other, as lists have to.)"""
+    b = Batch(19, [((61, 200), new + 20, new), ((), new, new), ((16,), 8, 1)], 8, 2, d, dtype)
+    t = b.up()
+    unwritten = b.slot // 16 % 2 == 0
+    unwritten[b.cu[:-1]] = True
+    t["slot_map"][torch.from_numpy(unwritten).cuda()] = _i32(np.resize([-1, b.n_blocks * 16, 2 ** 31 - 1, -2 ** 31], unwritten.sum()))
+    k0, v0 = t["k_pool"].clone(), t["v_pool"].clone()
+    ctx = _ctx(dtype, 8, 2, d)
+    assert unwritten.any() and not unwritten.all() and ctx.check_query_list(t["slot_map"], b.n_blocks) == 0
+    b.call(ctx, t)
+    torch.cuda.synchronize()
+    own = torch.zeros(b.n_blocks, 16, dtype=torch.bool, device="cuda")
+    own.view(-1)[torch.from_numpy(b.slot[~unwritten]).cuda()] = True
+    same = lambda x, y: torch.equal(torch.nan_to_num(x, nan=7.0), torch.nan_to_num(y, nan=7.0))
+    assert same(t["k_pool"].transpose(1, 2)[~own], k0.transpose(1, 2)[~own]) and same(t["v_pool"].permute(0, 3, 1, 2)[~own], v0.permute(0, 3, 1, 2)[~own])
+    assert torch.equal(t["v_pool"].permute(0, 3, 1, 2).reshape(-1, 2, d)[torch.from_numpy(b.slot[~unwritten]).cuda()].cpu(), b.v_new[torch.from_numpy(~unwritten)])
+    k, v, out = t["k_pool"].float().cpu().numpy(), t["v_pool"].float().cpu().numpy(), t["out"].double().cpu().numpy()
+    for r in range(b.n_req):
+        rows = range(b.cu[r], b.cu[r + 1])
+        o, _, bound, _ = A.attend(b.q[rows].double().numpy(), np.array(b.pos)[rows], *A.paged_context(k, v, lambda p: v[p], b.tab, b.segs, range(b.off[r], b.off[r + 1])),
+                                  THETA, 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24)
+        assert (np.abs(out[rows] - o) <= bound).all()
+
+
 def test_append_attention_in_graphs_that_share_a_workspace():
     """Two captured calls over one workspace, replayed in turn beside eager work, on a stream of their own."""
     batches = [Batch(12, SHAPES["draft"] + [((3000,), 4, 1)], 8, 2, 128, "bf16"), Batch(13, SHAPES["one each"], 8, 2, 128, "bf16")]
@@ -673,6 +700,20 @@ def test_sample_values_that_are_not_finite_in_long_rows(vocab, dtype):
               dict(top_k=150 * np.ones(9, int), top_p=0.9 * full, min_p=0.01 * full, temperature=0.7 * full)):
         for u in (rng.random(9, dtype=np.float32), np.full(9, 1 - 2.0 ** -24, np.float32), np.full(9, np.nan)):
             _check_sample(_sample(_ctx(), z, vocab, u, **s), z, vocab, u, **s)
+
+
+@pytest.mark.parametrize("vocab", [333, 13001])
+def test_sample_settings_at_their_ends(vocab):
+    """Temperatures from the smallest number to infinity and NaN, cuts next to off and to nothing, whole numbers at their limits."""
+    nan, inf, least = math.nan, math.inf, 2.0 ** -149
+    rows = [(t, k, p, m) for t in (least, 1e-30, 1e-3, 1e4, 1e38, inf, nan) for k, p, m in ((0, 1.0, 0.0), (7, 1.0, 0.0), (0, 0.37, 0.0), (9, 0.61, 0.0), (0, 1.0, 0.53))]
+    rows += [(1.0, 2 ** 31 - 1, 1.0, 0.0), (1.0, -2 ** 31, 1.0, 0.0), (1.0, 0, least, 0.0), (1.0, 0, nan, nan), (1.0, 0, inf, -inf), (1.0, 0, 1 - 2.0 ** -24, 0.0),
+             (0.9, 0, 1.0, least), (0.9, 0, 1.0, 1.0), (0.9, 0, 1.0, inf), (-inf, 3, 1.0, 0.0), (0.9, vocab, 1.0, 0.0), (0.9, vocab - 1, 1.0, 0.0)]
+    s = dict(zip(("temperature", "top_k", "top_p", "min_p"), (np.array(c) for c in zip(*rows))))
+    z = _logits(vocab, len(rows), vocab, "f32", 2)
+    for seed in range(3):
+        u = np.random.default_rng(seed).random(len(rows), dtype=np.float32)
+        _check_sample(_sample(_ctx(), z, vocab, u, **s), z, vocab, u, **s)
 
 
 def test_sample_without_the_optional_outputs_on_a_stream():
