@@ -50,6 +50,7 @@ class DecoderLoop:
         spare = w.n_requests * ((answer_tokens + 15) // 16 + 1) if answer_tokens else 0
         self.batch = DeviceBatch(w, device=device, impl=impl, spare_blocks=spare)
         b = self.batch
+        self.turn = 0                                                  # prefills and answers that have begun on the pages
         self.pages = [(b.k_req, b.v_req, b.v_map)] + [(b.k_req.clone(), b.v_req.clone(), b.v_map.clone())
                                                       for _ in weights[1:]] if answer_tokens else []
         up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(device).to(b.dt)
@@ -114,6 +115,7 @@ class DecoderLoop:
     def run(self, keep: bool = False):
         """Returns one record per layer (ms, rows; with keep also h_in, out, lse, h1, h2 as numpy arrays)."""
         b = self.batch
+        self.turn += 1
         self._shift(0)
         b.select()
         records = []
@@ -192,11 +194,17 @@ class AnswerLoop:
     cc_append_attention over the layer's pages -> cc_linear -> cc_rms_norm -> cc_gated_linear -> cc_linear, -> logits.
     embed [vocab, hidden], gain_out [hidden], w_out [vocab, hidden]: embedding, last normalisation, output projection (numpy).
     temperature, top_k, top_p, min_p: one value, or one per request; None: off.  stop: a request that draws this token
-    gets no further one; neither does one whose logits are all -infinity or NaN, or for which no row is left.  Nothing of a step depends on the host, so graph=True captures one and replays it."""
+    gets no further one; neither does one whose logits are all -infinity or NaN, or for which no row is left.  Nothing of a step
+    depends on the host, so graph=True captures one and replays it.
+    Another answer to the same prompts is another AnswerLoop, which takes the pages over: the one before it cannot go on."""
 
     def __init__(self, loop: DecoderLoop, embed, gain_out, w_out, eps: float = 1.0e-5, temperature=None, top_k=None, top_p=None,
                  min_p=None, stop: Optional[int] = None):
         assert loop.answer_tokens > 0, "the DecoderLoop must keep its pages (answer_tokens)"
+        if loop.turn == 0:
+            raise ValueError("AnswerLoop: the DecoderLoop has not run yet")
+        loop.turn += 1
+        self.turn = loop.turn
         self.loop, self.eps, self.stop = loop, float(eps), stop
         w, b = loop.w, loop.batch
         self.b, self.n = b, w.n_requests
@@ -294,6 +302,8 @@ class AnswerLoop:
     def run(self, u, graph: bool = False, keep: bool = False):
         """u [steps, requests]: the uniform numbers the tokens are drawn with (at most answer_tokens + 1 steps in all).  Returns the tokens [steps,
         requests] (-1: none, as the request has ended) and their log-probabilities (-infinity there); with keep also the logits each was drawn from."""
+        if self.turn != self.loop.turn:
+            raise ValueError("AnswerLoop: a later prefill or answer has taken the pages")
         u = torch.as_tensor(np.ascontiguousarray(u, dtype=np.float32)).to(self.u.device)
         if self.drawn + u.shape[0] > self.loop.answer_tokens + 1:
             raise ValueError("AnswerLoop: more tokens than the pages have room for")

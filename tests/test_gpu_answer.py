@@ -928,3 +928,25 @@ def test_answer_loop_ends_where_no_row_is_left(graph):
         for i in range(3):
             _ended(got, logprobs, free, i, n if i == r else 9)
         loop.close()
+
+
+def test_answer_loops_one_behind_the_other():
+    """A second answer from the same prefill is what it would be alone; the first cannot go on over its tokens, nor the second over another prefill's."""
+    from paper_2502_15734_amd.layers import AnswerLoop
+    u = np.random.default_rng(8).random((12, 3), dtype=np.float32)
+    _, _, loop, first, _, model = _answer_setup("bf16", temperature=1.0)
+    want, _ = first.run(u)
+    _, _, loop, first, _, model = _answer_setup("bf16", temperature=1.0)
+    first.run(np.flip(u)[:7])
+    second = AnswerLoop(loop, *model, temperature=1.0)
+    got, _ = second.run(u[:5])
+    with pytest.raises(ValueError, match="taken the pages"):
+        first.run(u[:1])
+    more, _ = second.run(u[5:])
+    assert np.array_equal(np.concatenate([got, more]), want)
+    loop.run()
+    with pytest.raises(ValueError, match="taken the pages"):
+        second.run(u[:1])
+    got, _ = AnswerLoop(loop, *model, temperature=1.0).run(u)
+    assert np.array_equal(got, want)
+    loop.close()
