@@ -307,6 +307,9 @@ class AnswerLoop:
         u = torch.as_tensor(np.ascontiguousarray(u, dtype=np.float32)).to(self.u.device)
         if self.drawn + u.shape[0] > self.loop.answer_tokens + 1:
             raise ValueError("AnswerLoop: more tokens than the pages have room for")
+        if u.shape[0] == 0:
+            none = np.zeros((0, self.n), dtype=np.int32), np.zeros((0, self.n), dtype=np.float32)
+            return none + ([],) if keep else none
         tokens, logprobs, logits, captured, fed = [], [], [], None, False
         for step in range(u.shape[0]):
             if self.drawn == 0:

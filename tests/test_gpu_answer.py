@@ -950,3 +950,12 @@ def test_answer_loops_one_behind_the_other():
     got, _ = AnswerLoop(loop, *model, temperature=1.0).run(u)
     assert np.array_equal(got, want)
     loop.close()
+
+
+def test_answer_loop_of_no_steps():
+    _, _, loop, ans, _, _ = _answer_setup("f32", answer=3, temperature=1.0)
+    u = np.random.default_rng(9).random((4, 3), dtype=np.float32)
+    first, then, behind = ans.run(u[:0]), ans.run(u, keep=True), ans.run(u[:0], keep=True)
+    assert first[0].shape == first[1].shape == (0, 3) and behind[0].shape == (0, 3) and behind[2] == [] and then[0].shape == (4, 3)
+    assert first[0].dtype == then[0].dtype and first[1].dtype == then[1].dtype
+    loop.close()
