@@ -471,9 +471,10 @@ class Context:
         if logits.dtype not in (torch.float32, torch.bfloat16):
             raise ValueError("sample: logits in float32 or bfloat16")
         n_rows = logits.shape[0]
-        for t in (u, token, temperature, top_k, top_p, min_p, logprob, n_kept):
-            if t is not None and t.shape[0] < n_rows:
-                raise ValueError("sample: a tensor has fewer entries than there are rows")
+        for t, kind in ((u, torch.float32), (token, torch.int32), (temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32),
+                        (min_p, torch.float32), (logprob, torch.float32), (n_kept, torch.int32)):
+            if t is not None and (t.shape[0] < n_rows or t.dtype != kind):
+                raise ValueError("sample: a tensor has fewer entries than there are rows, or another type than float32 (token, top_k, n_kept: int32)")
         self._check(self._lib.cc_sample(
             self._h, _ptr(logits), CC_BF16 if logits.dtype == torch.bfloat16 else CC_F32, n_rows, n_vocab, logits.shape[1],
             _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(token), _ptr(logprob), _ptr(n_kept), _ptr(workspace),

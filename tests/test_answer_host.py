@@ -169,3 +169,17 @@ def test_row_lists_beyond_the_grid_are_refused(lib):
     assert lib.cc_append_attention(one._h, good, good, good, None, good, good, good, (1 << 31) - 1, 1, good, good, 8, good, good, 1, good, 1, 100, 1, None,
                                    C.c_void_p(8192), None, good, (1 << 63) - 1, None) == -1 and b"2^24 - 1 workgroups" in lib.cc_last_error(one._h)
     one.close()
+
+
+def test_sample_refuses_tensors_of_other_types(lib):
+    """Numbers of 64 bits, numpy's own, would be read as others."""
+    import torch
+    import paper_2502_15734_amd as P
+    ctx = P.Context(8, 2, 128, 5.0e5, P.CC_BF16)
+    f, i = torch.zeros(4), torch.zeros(4, dtype=torch.int32)
+    ok = dict(u=f, token=i, temperature=f, top_k=i, top_p=f, min_p=f, logprob=f, n_kept=i)
+    for name, t in ok.items():
+        for bad in (t.double(), t.long(), t[:3]):
+            with pytest.raises(ValueError, match="fewer entries"):
+                ctx.sample(torch.zeros(4, 8), 8, **{**ok, name: bad})
+    ctx.close()
