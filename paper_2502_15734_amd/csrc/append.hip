@@ -14,9 +14,10 @@
 //
 // One pass: o = sum_t 2^(s_t - m) v_t and l = sum_t 2^(s_t - m), where the reference m of a column is shared by its lane groups and moves (o and l times
 // 2^(old - new)) only when a logit is more than kSlack above it.  m, l and o are fp32.  Queries, once they are turned to their position, and weights are what
-// the matrix instructions take: bf16 as the sum of two up to 64 columns, where the bytes of the keys are the bound (one row over 700 tokens 12.3 -> 12.7 us, 32
-// requests 115.2 -> 115.6, 16 x 5 rows of 64 heads 79.6 -> 82.6; rms error against 64 bits 0.0029 -> 0.0017 of the output, which is its own rounding), as one
-// above, where the products are (their rounding, 2^-9 of a weight at most, is that of the attention of the prefill).
+// the matrix instructions take: bf16 as the sum of two, so that the output's own rounding is the only one to 8 bits and a row's error does not depend on how many
+// rows its request brings (rms against 64 bits 0.0017 of the output, 0.0029 with one each).  Where the bytes of the keys are the bound that is next to free (one row
+// over 700 tokens 12.3 -> 12.7 us, 32 requests 115.2 -> 115.6, 16 x 5 rows of 64 heads 79.6 -> 82.6); where the products are, there are twice as many of them (500
+// rows over 16 000 tokens 158 -> 247; with two of the queries alone 197, of the weights alone 207, and 0.0024 either way).
 //
 // 32 heads on 8 of 128, bf16: 32 requests of one row over 1500 to 6700 tokens 115 us (4.5 TB/s of keys and values; a copy of 4 GiB moves 4.7), one
 // row over 130 000 tokens 105 us (5.1 TB/s), one over 700 tokens 12.7 us, of which two launches take 5 and the chain of dependent loads (segments, page
@@ -160,12 +161,12 @@ __device__ __forceinline__ void write_rows(const AppendArgs& a, const InvFreq& i
   __syncthreads();                                     // (the workgroup's loads behind it see the rows)
 }
 
-// x as a bf16, or as the sum of two.  Part 0 of two: the upper 16 bits of the number in front of x (towards 0), x becomes the rest.  So neither part of a number
-// is 0 - a product with an infinite factor is one infinity and not a difference of two or 0 x infinity - and both parts of 0 are: a masked key's
-// weight takes nothing of its value, however large.  The last part: the nearest bf16.  POSITIVE: x has no sign (NaN may).
-template <int PARTS, bool POSITIVE = false>
+// x as the sum of two bf16.  Part 0: the upper 16 bits of the number in front of x (towards 0), x becomes the rest, whose nearest bf16 is part 1.  So neither
+// part of a number is 0 - a product with an infinite factor is one infinity and not a difference of two or 0 x infinity - and both parts of 0 are: a masked
+// key's weight takes nothing of its value, however large.  POSITIVE: x has no sign (NaN may).
+template <bool POSITIVE = false>
 __device__ __forceinline__ bf16_t take_part(float& x, int part) {
-  if (part == PARTS - 1) return static_cast<bf16_t>(x);
+  if (part == 1) return static_cast<bf16_t>(x);
   const uint32_t sign = POSITIVE ? 0u : __float_as_uint(x) & 0x80000000u;
   const float up = __uint_as_float((__builtin_elementwise_sub_sat(__float_as_uint(x) ^ sign, 1u) & 0xffff0000u) | sign);
   x -= up;
@@ -212,7 +213,7 @@ template <int D> struct Tile<bf16_t, D> {
   static __device__ __forceinline__ Piece piece(float (&x)[8], int part) {
     Piece w;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = take_part<2, POSITIVE>(x[e], part);
+    for (int e = 0; e < 8; ++e) w[e] = take_part<POSITIVE>(x[e], part);
     return w;
   }
 };
@@ -474,9 +475,9 @@ __global__ __launch_bounds__(256, 2) void append_split_kernel(AppendArgs a, InvF
 // of pages; tiles of 64 keys go through LDS (two images, loads that write LDS while the other is multiplied, one barrier per tile), so that a page is read
 // once for all its columns.  CW = 4: each wavefront multiplies its 32 columns with all 64 keys; CW = 2: two wavefronts per 32 columns take 32
 // keys each and meet at the end.  Few columns are bound by the bytes (16 requests of 5 rows over 1000 to 8000 tokens, 64 heads on 8: 82 us, 3.6 TB/s), from some
-// hundred on by the vector instructions beside the matrix instructions: 500 rows of 32 heads over 16 000 tokens take 158 us, of them 140 to 150 in
-// this kernel, with the matrix cores busy for 54 % of its cycles, LDS for 30, and the rest in what lies between two products of a tile (maximum, mask,
-// barrier) that the other workgroup of the compute unit does not cover.
+// hundred on by the matrix instructions: 500 rows of 32 heads over 16 000 tokens take 247 us, of them about 230 in this kernel (264 GFLOP in two parts, 1.15 PF),
+// with the matrix cores busy for 72 % of its cycles, and the rest in what lies between two products of a tile (maximum, mask, barrier) that the
+// other workgroup of the compute unit does not cover.
 //
 // v_mfma_f32_32x32x16_bf16, S^T = K Q^T and O^T = V^T P^T with lane = (n = lane % 32, h = lane / 32), column n.  As above the key rows are
 // ordered so that a lane's logits are the tokens 8 h .. 8 h + 7 of each page: row 8 a + 4 b + c of a 32-key block is token
@@ -597,8 +598,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
 
   // ---- the queries at their positions, in units of the logits' powers of two
   const float scale = rsqrtf(static_cast<float>(D)) * kLog2e;
-  constexpr int kParts = CW == 2 ? 2 : 1;                             // (see the head of the file)
-  bf16x8 q[kParts][D / 16];
+  bf16x8 q[2][D / 16];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
     const bf16x8 x = __builtin_bit_cast(bf16x8, raw[i]), y = __builtin_bit_cast(bf16x8, raw[i + D / 32]);
@@ -609,9 +609,9 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
       const float u = to_float(x[e]), w = to_float(y[e]);
       float first = (u * cs - w * sn) * scale, second = (w * cs + u * sn) * scale;
 #pragma unroll
-      for (int part = 0; part < kParts; ++part) {
-        q[part][i][e] = take_part<kParts>(first, part);
-        q[part][i + D / 32][e] = take_part<kParts>(second, part);
+      for (int part = 0; part < 2; ++part) {
+        q[part][i][e] = take_part(first, part);
+        q[part][i + D / 32][e] = take_part(second, part);
       }
     }
   }
@@ -621,9 +621,6 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
   float m = 0.f, l = 0.f;
-  f32x16 from;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) from[e] = 0.f;
   float limit = -INFINITY;                                            // how far a logit may be above m: kSlack once the column has seen a key and m is a reference of its own
   // byte of this lane's key operand in an image: row of the block as token of its two pages; piece 2 kk + h is this one's, bits of kk flipped
   const int k_row = (n >> 4) * kBlock + ((n >> 2) & 1) * 8 + ((n >> 3) & 1) * 4 + (n & 3);
@@ -634,7 +631,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
   // steps are fenced, because the compiler by itself reads every operand right in front of its product and takes the exponentials together.
   auto compute = [&](auto set_aside, const u32x4* img, int i, int here, int flags) __attribute__((always_inline)) {
     constexpr bool ODD = decltype(set_aside)::value;
-    constexpr int kSteps = D / 16, kAhead = 4;   // products of a block; operands in flight
+    constexpr int kSteps = D / 16, kAhead = 2;   // pairs of products of a block; operands in flight
     const int b0 = ks * kBlocks;                                       // this wavefront's first 32-key block
     // (the operands' addresses are made here again: kept over the loop they would cost a register each)
     const char* bytes = reinterpret_cast<const char*>(img);
@@ -644,11 +641,10 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     auto value = [&](int b, int g, int j) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8*>(bytes + v_byte + (2 * b + g) * 32 * D + j * 512); };
     bf16x8 ahead[kAhead];                                              // operands of the next products, also over the masks and maxima between two blocks
     f32x16 s[kBlocks];
-    bf16x8 w[kBlocks][2], rest[2];                                     // (rest: of the weights, with two parts)
+    bf16x8 w[kBlocks][2], rest[kBlocks][2];                            // the weights' parts
     // the logits less the reference of the column, which enters as the products' first summand
     auto fence = []() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
-    auto first_summand = [&]() __attribute__((always_inline)) {          // (with two parts there are no registers to hold it)
-      if constexpr (kParts == 1) return from;
+    auto first_summand = [&]() __attribute__((always_inline)) {          // (there are no registers to hold it)
       f32x16 x;
 #pragma unroll
       for (int e = 0; e < 16; ++e) x[e] = -m;
@@ -659,12 +655,10 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
       float x0 = __builtin_amdgcn_exp2f(s[b][2 * x]), x1 = __builtin_amdgcn_exp2f(s[b][2 * x + 1]);
       l += x0;
       l += x1;
-      w[b][x / 4][2 * x % 8] = take_part<kParts, true>(x0, 0);
-      w[b][x / 4][2 * x % 8 + 1] = take_part<kParts, true>(x1, 0);
-      if constexpr (kParts == 2) {
-        rest[x / 4][2 * x % 8] = take_part<kParts, true>(x0, 1);
-        rest[x / 4][2 * x % 8 + 1] = take_part<kParts, true>(x1, 1);
-      }
+      w[b][x / 4][2 * x % 8] = take_part<true>(x0, 0);
+      w[b][x / 4][2 * x % 8 + 1] = take_part<true>(x1, 0);
+      rest[b][x / 4][2 * x % 8] = take_part<true>(x0, 1);
+      rest[b][x / 4][2 * x % 8 + 1] = take_part<true>(x1, 1);
     };
     // S(b); under it the weights of block `under` (-1: none)
     auto products = [&](int b, auto under) __attribute__((always_inline)) {
@@ -675,7 +669,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
 #pragma unroll
       for (int kk = 0; kk < kSteps; ++kk) {
         s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[kk % kAhead], q[0][kk], kk == 0 ? first_summand() : s[b], 0, 0, 0);
-        if constexpr (kParts == 2) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[kk % kAhead], q[1][kk], s[b], 0, 0, 0);
+        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[kk % kAhead], q[1][kk], s[b], 0, 0, 0);
         if (kk + kAhead < kSteps) ahead[kk % kAhead] = key(b, kk + kAhead);
         else if (!ODD && b + 1 < kBlocks) ahead[kk % kAhead] = key(b + 1, kk + kAhead - kSteps);
         else if (!ODD) ahead[kk % kAhead] = value(0, (kk + kAhead - kSteps) / (D / 32), (kk + kAhead - kSteps) % (D / 32));
@@ -687,9 +681,10 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
       if constexpr (decltype(under)::value >= 0)
 #pragma unroll
         for (int g = 0; g < 2; ++g) {                                  // (the weights are made here, not behind the next branch)
-          u32x4 bits = __builtin_bit_cast(u32x4, w[decltype(under)::value][g]);
-          asm volatile("" : "+v"(bits));
+          u32x4 bits = __builtin_bit_cast(u32x4, w[decltype(under)::value][g]), low = __builtin_bit_cast(u32x4, rest[decltype(under)::value][g]);
+          asm volatile("" : "+v"(bits), "+v"(low));
           w[decltype(under)::value][g] = __builtin_bit_cast(bf16x8, bits);
+          rest[decltype(under)::value][g] = __builtin_bit_cast(bf16x8, low);
         }
     };
     // masks, and the reference where a logit lies too far above it; done: blocks whose weights are made but not multiplied yet
@@ -716,8 +711,6 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
         m += top;
         l *= f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) from[e] = -m;
-#pragma unroll
         for (int j = 0; j < D / 32; ++j) o[j] *= f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[b][e] -= top;
@@ -726,7 +719,11 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
 #pragma unroll
           for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[d][g][e] = static_cast<bf16_t>(to_float(w[d][g][e]) * f);
+            for (int e = 0; e < 8; ++e) {
+              float x = (to_float(w[d][g][e]) + to_float(rest[d][g][e])) * f;
+              w[d][g][e] = take_part<true>(x, 0);
+              rest[d][g][e] = take_part<true>(x, 1);
+            }
       }
     };
     // o += V P(b); under it the weights of block `under`
@@ -737,10 +734,10 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
 #pragma unroll
         for (int x = 0; x < kV; ++x) {
           const int j = x % (D / 32);
-          o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[x % 4], w[b][x / (D / 32)], o[j], 0, 0, 0);
-          if constexpr (kParts == 2) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[x % 4], rest[x / (D / 32)], o[j], 0, 0, 0);
-          if (x + 4 < kV) ahead[x % 4] = value(b, (x + 4) / (D / 32), (x + 4) % (D / 32));
-          else if (b + 1 < kBlocks) ahead[x % 4] = value(b + 1, (x + 4 - kV) / (D / 32), (x + 4 - kV) % (D / 32));
+          o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[x % kAhead], w[b][x / (D / 32)], o[j], 0, 0, 0);
+          o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[x % kAhead], rest[b][x / (D / 32)], o[j], 0, 0, 0);
+          if (x + kAhead < kV) ahead[x % kAhead] = value(b, (x + kAhead) / (D / 32), (x + kAhead) % (D / 32));
+          else if (b + 1 < kBlocks) ahead[x % kAhead] = value(b + 1, (x + kAhead - kV) / (D / 32), (x + kAhead - kV) % (D / 32));
           if constexpr (decltype(under)::value >= 0)
 #pragma unroll
             for (int y = 0; y < 8 / kV; ++y) weigh(decltype(under)::value, x * (8 / kV) + y);
@@ -756,7 +753,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = fabsf(to_float(v[e])) < INFINITY ? v[e] : static_cast<bf16_t>(0.f);
             o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[b][g], o[j], 0, 0, 0);
-            if constexpr (kParts == 2) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, rest[g], o[j], 0, 0, 0);
+            o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, rest[b][g], o[j], 0, 0, 0);
           }
           const int pg = (b0 + b) * 2 + g, first = list[i + pg].pos0;
           const bf16_t* values = reinterpret_cast<const bf16_t*>(img + 8 * D + pg * 2 * D);
@@ -766,7 +763,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
             asm volatile("" : "+v"(dim0));
             float weight = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) weight = t % 8 == e ? to_float(w[b][g][e]) + (kParts == 2 ? to_float(rest[g][e]) : 0.f) : weight;
+            for (int e = 0; e < 8; ++e) weight = t % 8 == e ? to_float(w[b][g][e]) + to_float(rest[b][g][e]) : weight;
             weight = __shfl(weight, n + 32 * (t >> 3), 64);
             const bool sees = first + t <= pos;
 #pragma unroll
@@ -789,7 +786,7 @@ __global__ __launch_bounds__(256, 2) void append_tile_kernel(AppendArgs a, InvFr
     settle(0, 0);
     if constexpr (kBlocks == 2 && !ODD) {
       // (ahead of the compute unit's other workgroup while exponentials and products go together, behind it where there are products alone: 500 rows
-      // over 16 000 tokens 160.8 -> 157, with the whole tile ahead; 165 without)
+      // over 16 000 tokens 252 -> 247)
       __builtin_amdgcn_s_setprio(1);
       products(1, first_block);
       settle(1, 1);
@@ -953,7 +950,7 @@ __global__ __launch_bounds__(256) void append_join_kernel(AppendArgs a, int n_it
 // How the work of a call is divided: from host scalars alone.  What either side of a choice takes (16 requests of 1000 to 8000 tokens, 64 heads on 8, if
 // nothing else is said):
 //   columns of a workgroup   up to 16: append_split_kernel; 32 columns as two groups of it 112 us, as one of 64 columns of append_tile_kernel 78.
-//                            up to 64, then 128: 72 columns as two groups of 64 116 us, as one of 128 87
+//                            up to 64, then 128: 72 columns as two groups of 64 135 us, as one of 128 116
 //   ranges                   about 512 workgroups, two on a compute unit: the tile kernel with 256 97 us, with 512 76, with 1024 92; the split kernel 70, 73, 82
 //                            (and 32 requests of one row 118, 115, 125).  The split kernel's number is the nearest, the tile kernel's rounded down: 24
 //                            requests with 1.3 workgroups a unit 83 us, with 2 70; 40 requests of 8 rows with 1.25 145 us, with 2.5 164

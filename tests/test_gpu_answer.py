@@ -312,6 +312,25 @@ def test_append_attention_few_columns_lose_nothing_inside(hq, d, new):
         assert (np.abs(out[rows] - o) <= bound).all(), f"request {r}: {(np.abs(out[rows] - o) / bound).max():.3g} of the bound"
 
 
+@pytest.mark.parametrize("scale", [1.0, 3.0])
+@pytest.mark.parametrize("hq,d,new", [(8, 128, 17), (8, 64, 40), (12, 128, 45), (2, 128, 140), (16, 64, 33)])
+def test_append_attention_many_columns_lose_nothing_inside(hq, d, new, scale):
+    """As above for more than 64 rows and heads on a KV head; scale: with larger logits the reference of a row moves, and weights with it."""
+    b = Batch(20, [((700, 33), new + 5, new), ((), new + 40, new), ((250,), new, new)], hq, 2, d, "bf16", scale=scale)
+    t = b.up()
+    b.call(_ctx("bf16", hq, 2, d), t)
+    torch.cuda.synchronize()
+    k, v, out = t["k_pool"].float().cpu().numpy(), t["v_pool"].float().cpu().numpy(), t["out"].double().cpu().numpy()
+    for r in range(b.n_req):
+        rows = range(b.cu[r], b.cu[r + 1])
+        context = A.paged_context(k, v, lambda p: v[p], b.tab, b.segs, range(b.off[r], b.off[r + 1]))
+        q = b.q[rows].double().numpy()
+        o, _, bound, _ = A.attend(q, np.array(b.pos)[rows], *context, THETA, 2.0 ** -15)
+        turn = 4e-6 * np.abs(q).max() * np.abs(context[1]).sum(-1).max() / math.sqrt(d)
+        bound += 2.0 ** -8 * np.abs(o) + math.expm1(2 * turn) * np.abs(context[2]).max()
+        assert (np.abs(out[rows] - o) <= bound).all(), f"request {r}: {(np.abs(out[rows] - o) / bound).max():.3g} of the bound"
+
+
 @pytest.mark.parametrize("dtype,d,new", [("bf16", 128, 1), ("bf16", 64, 4), ("bf16", 128, 5), ("bf16", 64, 16), ("bf16", 128, 40), ("f32", 128, 3)])
 def test_append_attention_infinite_values_that_every_row_sees(dtype, d, new):
     """An infinite value has a weight above 0 in every row: that dimension is infinite, the others are what they are without it.  One request has a
