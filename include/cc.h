@@ -500,8 +500,12 @@ int cc_extend_segments(cc_ctx* ctx, const cc_segment* segs_in, const int32_t* n_
 /* ---- (g) attention of new rows over the paged context ------------------------------------------
  * cc_sparse_prefill for the rows of an answer: one per request while it is written, several for a draft that is
  * checked at once, some hundred for a further question over a long context.  The same two steps and the same
- * arguments (rows, positions and slots from cc_extend_segments or any list cc_sparse_prefill takes), but the KEYS are
- * divided over workgroups, and the parts joined, so that a few rows of a long context fill the chip.
+ * arguments (rows, positions and slots from cc_extend_segments or any list cc_sparse_prefill takes; a request's segments in
+ * prompt order, so that positions ascend from page to page), but the KEYS are divided over workgroups, and the parts
+ * joined, so that a few rows of a long context fill the chip.
+ *   bf16: turned queries and softmax weights are sums of two bf16, the output's rounding is the only one to 8 bits.
+ *   cc_sparse_prefill rounds both to one bf16 (rms error 0.0029 of the output instead of 0.0017) and takes less time where
+ *   rows are many: from 64 rows a request on if there are several requests, from some hundred if there is one.
  *   slot_map[j] is the slot of row j's own token, in a page of its request, or lies outside the pool: the row is then
  *   attended but not written.  As for cc_sparse_prefill the rows of one page follow each other (one that is not written
  *   parts them: cc_check_query_list).  Rows [cu_q[n_requests], n_q_tot) are not attended, their out and lse stay as they are, and
@@ -535,7 +539,7 @@ int cc_append_attention(cc_ctx* ctx, const void* q, const void* k_new, const voi
  *     top_p:  weight of the ranks in front < top_p[r] * weight of the ranks that pass top_k     (1 or more: off)
  *     min_p:  w_i >= min_p[r]                                           (0 or less: off)
  *   and rank 0 in any case.  token[r] = the first kept token i, by index, with  sum_{kept j <= i} w_j > u[r] * sum_kept w.
- *   temperature[r] <= 0: the largest logit (lowest index), whatever the other settings.
+ *   temperature[r] <= 0 or NaN: the largest logit (lowest index), whatever the other settings.  A NaN in top_p or min_p: off.
  *   logprob[r] = log(w_token / sum_kept w);  n_kept[r] = number of kept tokens.
  * -infinity and NaN are never kept; a row of nothing else gives token -1, logprob -infinity, n_kept 0.  Beside +infinity
  * every finite logit has weight 0.  u below 0 or NaN counts as 0, u of 1 or more as the largest float below 1.

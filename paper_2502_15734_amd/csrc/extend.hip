@@ -7,7 +7,7 @@
 // Bound by latency: a step of some hundred answers reads and writes some ten kilobytes, and a launch costs more than that.  So batches
 // whose tables fit a workgroup's LDS are one launch of one workgroup (extend_small_kernel); others are a launch for the needs, one that
 // places the segments (every workgroup scans all needs again, which is cheaper than a launch between) and one for the rows.
-// 32 requests of one row each (5 to 10 segments) 7.5 us, where a launch alone takes 2.4; 250 requests, some with a question, 13.8; the tables of 500 whole
+// 32 requests of one row each (5 to 10 segments) 7.7 us, where a launch alone takes 2.4; 250 requests, some with a question, 13.9; the tables of 500 whole
 // prompts, 2.8 million rows, 22 us (1.6 TB/s, of which a third is the chain through the two kernels in front).
 #include <algorithm>
 
