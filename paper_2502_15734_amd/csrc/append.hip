@@ -1035,7 +1035,7 @@ __global__ __launch_bounds__(64) void append_scalar_kernel(
   if (lse != nullptr && lane == 0) lse[static_cast<size_t>(j) * hq + h] = z == 0.f ? -INFINITY : m + logf(z);
 }
 
-// Join of the ranges: up to eight by as many rows and heads a workgroup as it has groups of D / 4 threads, more by a workgroup each.
+// The join: a workgroup for 1024 / D rows and heads, or, where there are more than eight ranges, for each (see append_join_kernel).
 static bool join_is_wide(const AppendPlan& p) { return p.n_splits > 8; }
 static long long join_groups(const AppendPlan& p, long long n_items, int d) {
   const int per = join_is_wide(p) ? 1 : 1024 / d;
