@@ -18,8 +18,8 @@
 // same steps there.
 //
 // Few rows are bound by latency: four launches, each with a chain of two or three loads, scans and barriers (1 x 32000 fp32 with top-p 23.3 us, of
-// which the last kernel takes 7; 32 x 128256 bf16 36 to 39 us).  Many rows are bound by the three reads and the arithmetic in 64 bits beside the second and third:
-// 256 x 128001 fp32 (131 MB) with all kinds of settings 104 us: 26 for the first pass (5 TB/s), 27, 37 and 10 to 23 for the last kernel, the
+// which the last kernel takes 7; 32 x 128256 bf16 35 to 39 us).  Many rows are bound by the three reads and the arithmetic in 64 bits beside the second and third:
+// 256 x 128001 fp32 (131 MB) with all kinds of settings 104 to 111 us: 26 for the first pass (5 TB/s), 27, 37 and 10 to 23 for the last kernel, the
 // longest where a row has many candidates to sort.
 #include <algorithm>
 
